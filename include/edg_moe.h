@@ -407,6 +407,41 @@ int32_t moe_expert_ffn_int4_lora_static(const edg_layer_desc* desc, const void* 
                                         const int32_t* experts, const float* gates, const void* x,
                                         const edg_lora* lora, void* y, void* stream);
 
+/* ---------------------------------------------------------------- int4 projections */
+
+/* One projection of a decoder block outside the experts (queries, latent rows, attention output, output head): W [N][Kd] in the
+ * weight format above, with the unmerged adapter of the experts (Sec. 3.3; Sec. 4 "Phase 2" attaches it to the attention
+ * projections):   y[t] = W x[t] + lora_scale * B (A x[t]). */
+typedef struct edg_linear_desc {
+    int32_t N;           /* output rows, any number from 1 to 2^24                               */
+    int32_t Kd;          /* input dimension: a multiple of group, at most 65536                  */
+    int32_t group;       /* quantisation group size along the input dimension: a multiple of 32  */
+    int32_t rank;        /* LoRA rank r, 0 (no adapter) to 64                                    */
+    int32_t out_dtype;   /* type of y: EDG_F32, EDG_F16 or EDG_BF16                              */
+    int32_t ldx;         /* elements from one row of x to the next, a multiple of 8; 0 = Kd      */
+    int32_t ldy;         /* elements from one row of y to the next; 0 = N                        */
+    float   lora_scale;  /* alpha / r                                                            */
+} edg_linear_desc;
+
+/* Bytes of the record of a projection; the device copy must be 256-byte aligned. */
+int32_t edg_linear_record_bytes(const edg_linear_desc* desc, size_t* bytes);
+
+/* One-time host repack of canonical tensors (codes [N][Kd/2], scales and zeros fp16 bits [N][Kd/group]) into the record the
+ * kernels read, and its exact inverse.  Same rule for zero points as edg_pack_expert (EDG_E_RANGE, nothing written). */
+int32_t edg_pack_linear(const edg_linear_desc* desc, const uint8_t* codes, const uint16_t* scales, const uint16_t* zeros, void* record);
+int32_t edg_unpack_linear(const edg_linear_desc* desc, const void* record, uint8_t* codes, uint16_t* scales, uint16_t* zeros);
+
+/* Bytes of device scratch for T tokens (A x of every token; never zero, and never falling as T grows). */
+int32_t edg_linear_workspace_bytes(const edg_linear_desc* desc, int32_t T, size_t* bytes);
+
+/* record dev; x dev bf16 [T][ldx], each row 16-byte aligned; A dev bf16 [rank][Kd] and B dev bf16 [N][rank], 16-byte aligned (read only
+ * with rank > 0); y dev [T][ldy] of out_dtype, aligned to its type (columns N.. of a row are not touched); workspace 256-byte aligned, needs no
+ * initialisation; calls that share one must be ordered on the device.  1 <= T <= 65535; made for batched decode: the weights are
+ * read once for every 64 tokens.  Codes enter the products exactly, activations as fp16 beside a power of two per token (2^-34 of the
+ * largest one is lost), sums are fp32. */
+int32_t linear_int4_lora(const edg_linear_desc* desc, const void* record, int32_t T, const void* x, const void* A, const void* B,
+                         void* y, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------- the whole layer-step */
 
 /* One layer-step of batch-1 decode (Sec. 3.2 "Motivation": the double shift).  On `stream`:

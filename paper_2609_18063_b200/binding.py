@@ -18,7 +18,8 @@ __all__ = [
     "make_desc", "make_lora", "version", "check_desc", "record_bytes", "pack_expert", "unpack_expert",
     "ffn_workspace_bytes", "workspace_status", "set_trace_buffer", "prerouter_topk", "prerouter_topk_tokens", "softmax_topk_rows", "sigmoid_group_topk_rows", "prerouter_mlp_topk",
     "moe_expert_ffn_int4_lora", "moe_expert_ffn_int4_lora_static", "moe_layer_decode", "stage_experts_to_slots",
-    "moe_layer_decode_dependent", "stack_decode_token", "next_hidden_state", "EXPORTS",
+    "moe_layer_decode_dependent", "stack_decode_token", "next_hidden_state", "LinearDesc", "make_linear_desc", "linear_record_bytes", "pack_linear",
+    "unpack_linear", "linear_workspace_bytes", "linear_int4_lora", "EXPORTS",
 ]
 
 F32, F16, BF16 = 0, 1, 2
@@ -49,6 +50,10 @@ class EdgError(RuntimeError):
 class LayerDesc(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("H", "I", "E", "K", "group", "rank", "n_adapters", "n_slots",
                                           "pre_dtype", "out_dtype")] + [("lora_scale", C.c_float)]
+
+
+class LinearDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("N", "Kd", "group", "rank", "out_dtype", "ldx", "ldy")] + [("lora_scale", C.c_float)]
 
 
 class Lora(C.Structure):
@@ -93,6 +98,7 @@ class StoreStats(C.Structure):
 
 _P = C.c_void_p
 _D = C.POINTER(LayerDesc)
+_DL = C.POINTER(LinearDesc)
 _SIG = {
     "edg_version": ([], C.c_int32),
     "edg_last_cuda_error": ([], C.c_int32),
@@ -131,6 +137,11 @@ _SIG = {
     "stage_experts_to_slots": ([_P, C.c_int32, _P, C.c_int32, _P, C.POINTER(C.c_int32)], C.c_int32),
     "moe_expert_ffn_int4_lora": ([_D, _P, _P, C.c_int32, _P, _P, _P, _P, C.POINTER(Lora), _P, _P, C.c_size_t, _P], C.c_int32),
     "moe_expert_ffn_int4_lora_static": ([_D, _P, _P, _P, _P, _P, _P, C.POINTER(Lora), _P, _P], C.c_int32),
+    "edg_linear_record_bytes": ([_DL, C.POINTER(C.c_size_t)], C.c_int32),
+    "edg_pack_linear": ([_DL] + [_P] * 4, C.c_int32),
+    "edg_unpack_linear": ([_DL] + [_P] * 4, C.c_int32),
+    "edg_linear_workspace_bytes": ([_DL, C.c_int32, C.POINTER(C.c_size_t)], C.c_int32),
+    "linear_int4_lora": ([_DL, _P, C.c_int32, _P, _P, _P, _P, _P, C.c_size_t, _P], C.c_int32),
     "moe_layer_decode": ([_P, C.c_int32, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, C.c_size_t, _P], C.c_int32),
 }
 EXPORTS = tuple(_SIG)
@@ -176,8 +187,8 @@ def _stream(stream) -> Optional[int]:
 
 _edgcall.init({n: C.cast(getattr(_lib, n), C.c_void_p).value for n in (
     "prerouter_topk", "prerouter_topk_tokens", "softmax_topk_rows", "sigmoid_group_topk_rows", "prerouter_mlp_topk",
-    "moe_expert_ffn_int4_lora", "moe_layer_decode", "moe_layer_decode_dependent", "edg_stack_decode_token", "edg_next_hidden_state")},
-    _ptr, _stream, _check, LayerDesc, Lora, C.c_int32, C.c_size_t)
+    "moe_expert_ffn_int4_lora", "moe_layer_decode", "moe_layer_decode_dependent", "edg_stack_decode_token", "edg_next_hidden_state", "linear_int4_lora")},
+    _ptr, _stream, _check, LayerDesc, Lora, LinearDesc, C.c_int32, C.c_size_t)
 
 
 _DT = {"f32": F32, "f16": F16, "bf16": BF16}
@@ -315,6 +326,49 @@ def moe_expert_ffn_int4_lora_static(desc, slot_pool, slot_table, slots, experts,
                                                 _ptr(experts), _ptr(gates), _ptr(x),
                                                 None if lora is None else C.byref(lora), _ptr(y), _stream(stream)),
            "moe_expert_ffn_int4_lora_static")
+
+
+def make_linear_desc(N, Kd, *, group=64, rank=0, out_dtype="f32", lora_scale=1.0, ldx=0, ldy=0) -> LinearDesc:
+    """Descriptor of one int4 projection W [N][Kd]; ldx / ldy: elements between rows of x and y (0 = dense)."""
+    return LinearDesc(int(N), int(Kd), int(group), int(rank), _DT[out_dtype] if isinstance(out_dtype, str) else int(out_dtype), int(ldx), int(ldy),
+                      float(lora_scale))
+
+
+def linear_record_bytes(desc: LinearDesc) -> int:
+    n = C.c_size_t()
+    _check(_lib.edg_linear_record_bytes(C.byref(desc), C.byref(n)), "edg_linear_record_bytes")
+    return n.value
+
+
+def pack_linear(desc: LinearDesc, codes, scales, zeros, record=None) -> np.ndarray:
+    """Canonical codes u8 [N][Kd/2], scales and zeros f16 [N][Kd/group] -> record (numpy uint8, or written into `record`)."""
+    arrs = [np.ascontiguousarray(codes, dtype=np.uint8)] + [np.ascontiguousarray(np.asarray(a, dtype=np.float16).view(np.uint16)) for a in (scales, zeros)]
+    size = linear_record_bytes(desc)                    # (checks the descriptor)
+    groups = (desc.N, desc.Kd // desc.group)
+    if arrs[0].shape != (desc.N, desc.Kd // 2) or arrs[1].shape != groups or arrs[2].shape != groups:
+        raise ValueError("tensor shapes do not match the descriptor")
+    if record is None:
+        record = np.empty(size, dtype=np.uint8)
+    _check(_lib.edg_pack_linear(C.byref(desc), *[_ptr(a) for a in arrs], _ptr(record)), "edg_pack_linear")
+    return record
+
+
+def unpack_linear(desc: LinearDesc, record):
+    groups = (desc.N, desc.Kd // max(desc.group, 1))
+    codes, sc, ze = np.empty((desc.N, desc.Kd // 2), np.uint8), np.empty(groups, np.uint16), np.empty(groups, np.uint16)
+    _check(_lib.edg_unpack_linear(C.byref(desc), _ptr(record), _ptr(codes), _ptr(sc), _ptr(ze)), "edg_unpack_linear")
+    return codes, sc.view(np.float16), ze.view(np.float16)
+
+
+def linear_workspace_bytes(desc: LinearDesc, T: int = 1) -> int:
+    n = C.c_size_t()
+    _check(_lib.edg_linear_workspace_bytes(C.byref(desc), T, C.byref(n)), "edg_linear_workspace_bytes")
+    return n.value
+
+
+def linear_int4_lora(desc, record, T, x, A, B, y, workspace, workspace_bytes=None, stream=None) -> None:
+    """y[t] = W x[t] + lora_scale B (A x[t]); A and B None without an adapter."""
+    _edgcall.linear_int4_lora(desc, record, T, x, A, B, y, workspace, workspace_bytes, stream)
 
 
 class Store:

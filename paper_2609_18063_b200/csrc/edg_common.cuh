@@ -68,6 +68,24 @@ cudaError_t launch_pdl(void (*kern)(Params...), dim3 grid, int threads, size_t s
     return launch_pdl_cluster(1, kern, grid, threads, smem, st, args...);
 }
 
+// An ordinary launch in clusters of `cluster` CTAs along x.
+template <typename... Params, typename... Args>
+cudaError_t launch_cluster(int cluster, void (*kern)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = (unsigned)cluster;
+    at.val.clusterDim.y = 1;
+    at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = cluster > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 // ---------------------------------------------------------------- record layout
@@ -548,6 +566,12 @@ __device__ __forceinline__ void mirror_inds(int32_t* mirror, const int32_t* inds
 template <typename T> __device__ __forceinline__ void store_out(T* y, size_t i, float v);
 template <> __device__ __forceinline__ void store_out<float>(float* y, size_t i, float v) { y[i] = v; }
 template <> __device__ __forceinline__ void store_out<__half>(__half* y, size_t i, float v) { y[i] = __float2half_rn(v); }
+// bits of v as bf16, rounded to nearest even; NaN stays NaN
+__device__ __forceinline__ uint16_t bf16_rn(float v) {
+    uint16_t b;
+    asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(b) : "f"(v));
+    return b;
+}
 struct bf16_t { uint16_t bits; };
 template <> __device__ __forceinline__ void store_out<bf16_t>(bf16_t* y, size_t i, float v) {
     uint32_t u = __float_as_uint(v);

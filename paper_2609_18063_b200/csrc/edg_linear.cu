@@ -1,0 +1,435 @@
+// y[t] = W x[t] + lora_scale B (A x[t]): one int4 projection for a few tokens.
+//
+//     y[t,n] = sum over groups of s[n,g] ( sum_k q[n,k] x[t,k] - z[n,g] sum_k x[t,k] )  +  lora_scale sum_r B[n,r] u[t,r],   u = A x
+//
+// Memory bounds it (N Kd / 2 bytes of codes for 2 T N Kd operations), so the design is about reading the codes at full width and
+// doing little per code.  The codes are the A operand of m16n8k16 tensor-core products (16 rows), eight tokens the B operand; the
+// codes go in as the fp16 subnormals that their bits are (edg_mma.cuh: five instructions for eight codes), the activations
+// carry a power of two per token.  Sums of one group leave the accumulator with the zero point removed and the scale applied, in fp32.
+//
+// Record: codes [N/16 row tiles][Kd/128 blocks][2][32 lanes][16 bytes] -- lane 4g + t of half h holds, chunk by chunk (32 codes) of the
+// block, the t-th word of row g + 8h, which is its operand of the product: a block of a row tile is two coalesced 16-byte loads a lane.
+// Then (scale, zero) [N/16][Kd/128][16 rows][128/GS] with GS = 32, 64 or 128 codes to a pair (the largest of these that divides the group:
+// the kernel then knows how many pairs a block has, one load a row).  Rows and codes beyond N and Kd are zero.
+//
+// A warp walks the blocks of its row tile, four of them in flight in registers; the warps of a CTA share a row tile's blocks
+// (WK of them) or take row tiles of their own, and a cluster of CTAs shares the input dimension where the row tiles alone do not fill
+// the GPU.  Partial sums meet in shared memory (of the cluster's first CTA), in a fixed order.
+#include <string.h>
+
+#include "edg_mma.cuh"
+#include "edg_ptx.cuh"
+
+namespace edg {
+
+bool zero_points_ok(const uint16_t* z, size_t n);      // edg_pack.cu
+
+namespace {
+
+constexpr int kThreads = 256, kWarps = 8;
+constexpr int kAhead = 4;                     // blocks of codes in flight per warp
+
+inline int pair_codes(int group) { return group % 128 == 0 ? 128 : (group % 64 == 0 ? 64 : 32); }
+inline int blocks_of(int Kd) { return (Kd + 127) / 128; }
+inline size_t tiles_of(int N) { return ((size_t)N + 15) / 16; }
+inline size_t codes_bytes(const edg_linear_desc& d) { return tiles_of(d.N) * blocks_of(d.Kd) * 1024; }
+inline size_t record_size(const edg_linear_desc& d) { return codes_bytes(d) + tiles_of(d.N) * blocks_of(d.Kd) * 64 * (128 / pair_codes(d.group)); }
+
+int32_t check(const edg_linear_desc* d) {
+    if (d == nullptr) return EDG_E_INVAL;
+    if (d->N < 1 || d->N > (1 << 24) || d->Kd < 32 || d->Kd > 65536) return EDG_E_SHAPE;
+    if (d->group < 32 || d->group % 32 != 0 || d->Kd % d->group != 0) return EDG_E_SHAPE;
+    if (d->rank < 0 || d->rank > 64) return EDG_E_SHAPE;
+    if (d->out_dtype != EDG_F32 && d->out_dtype != EDG_F16 && d->out_dtype != EDG_BF16) return EDG_E_INVAL;
+    if (d->ldx != 0 && (d->ldx < d->Kd || d->ldx % 8 != 0)) return EDG_E_SHAPE;
+    if (d->ldy != 0 && d->ldy < d->N) return EDG_E_SHAPE;
+    return EDG_OK;
+}
+
+// canonical <-> record.  Codes of a word keep their order: code k of it in bits 4k..4k+3.
+void repack_linear(const edg_linear_desc& d, uint8_t* rec, uint8_t* codes, uint16_t* sc, uint16_t* ze, bool to_record) {
+    const int nb = blocks_of(d.Kd), gs = pair_codes(d.group), per = 128 / gs;
+    uint8_t* rz = rec + codes_bytes(d);
+    for (int n = 0; n < d.N; ++n) {
+        const size_t tile = n >> 4;
+        const int row = n & 15, half = row >> 3, g = row & 7;
+        for (int w = 0; w < d.Kd / 8; ++w) {                  // word w of the row: chunk w / 4, lane w % 4 of the quad
+            const int b = w >> 4, chunk = (w >> 2) & 3, t = w & 3;
+            uint8_t* r = rec + ((tile * nb + b) * 2 + half) * 512 + (g * 4 + t) * 16 + chunk * 4;
+            uint8_t* c = codes + (size_t)n * (d.Kd / 2) + (size_t)w * 4;
+            if (to_record) memcpy(r, c, 4); else memcpy(c, r, 4);
+        }
+        for (int p = 0; p < d.Kd / gs; ++p) {
+            uint16_t* r = reinterpret_cast<uint16_t*>(rz + (((tile * nb + p / per) * 16 + row) * per + p % per) * 4);
+            const size_t k = (size_t)n * (d.Kd / d.group) + (size_t)p * gs / d.group;
+            if (to_record) { r[0] = sc[k]; r[1] = ze[k]; } else { sc[k] = r[0]; ze[k] = r[1]; }
+        }
+    }
+}
+
+struct LinearParams {
+    const uint8_t* codes;
+    const uint8_t* sz;
+    const uint16_t* x;
+    const float* u;             // [T][rank] or null
+    const uint16_t* B;
+    void* y;
+    int N, Kd, T, rank, out_dtype, ldx;
+    size_t ldy;
+    int tiles, blocks;          // row tiles; blocks of 128 codes of the input dimension
+    int wk;                     // warps that share a row tile; kWarps / wk row tiles to a unit
+    int cluster, cta_blocks;    // CTAs that share the input dimension; blocks of each
+    float lora_scale;
+};
+
+// u[t][r] = A[r] . x[t]: a warp per (token, rank)
+__global__ void __launch_bounds__(128) linear_u_kernel(const uint16_t* A, const uint16_t* x, float* u, int Kd, int ldx, int rank) {
+    pdl_launch_dependents();
+    const int r = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31, t = blockIdx.y;
+    if (r >= rank) return;
+    const uint4* a = reinterpret_cast<const uint4*>(A + (size_t)r * Kd);
+    const uint4* b = reinterpret_cast<const uint4*>(x + (size_t)t * ldx);
+    float s = 0.f;
+#pragma unroll 4
+    for (int i = lane; i < Kd / 8; i += 32) {
+        const uint4 v = __ldg(a + i), w = __ldg(b + i);
+        s = fmaf(bf16_lo(v.x), bf16_lo(w.x), s); s = fmaf(bf16_hi(v.x), bf16_hi(w.x), s);
+        s = fmaf(bf16_lo(v.y), bf16_lo(w.y), s); s = fmaf(bf16_hi(v.y), bf16_hi(w.y), s);
+        s = fmaf(bf16_lo(v.z), bf16_lo(w.z), s); s = fmaf(bf16_hi(v.z), bf16_hi(w.z), s);
+        s = fmaf(bf16_lo(v.w), bf16_lo(w.w), s); s = fmaf(bf16_hi(v.w), bf16_hi(w.w), s);
+    }
+    s = warp_sum(s);
+    if (lane == 0) u[(size_t)t * rank + r] = s;
+}
+
+// Shared memory: activations [blocks][4 chunks][NT][32 lanes] 16 bytes; sums of them [blocks][128/GS][NT * 8] float; scales of the tokens
+// [NT * 8]; partial sums [kWarps][16 rows][NT * 8] float.
+template <int GS, int NT> constexpr size_t linear_smem(int blocks) {
+    return (size_t)blocks * (NT * 2048 + (128 / GS) * NT * 32) + NT * 8 * 4 + kWarps * 16 * NT * 8 * 4;
+}
+
+// CTAs that share an SM, by the registers of NT tiles of tokens
+template <int NT> constexpr int kResident = NT <= 2 ? 2 : 1;
+
+template <int GS, int NT>
+__global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const __grid_constant__ LinearParams p) {
+    constexpr int PB = 128 / GS;                       // (scale, zero) pairs of a row in a block
+    constexpr int TN = NT * 8;
+    extern __shared__ __align__(16) uint8_t smem[];
+    uint4* s_x = reinterpret_cast<uint4*>(smem);
+    float* s_sum = reinterpret_cast<float*>(smem + (size_t)p.cta_blocks * NT * 2048);
+    float* s_scale = s_sum + (size_t)p.cta_blocks * PB * TN;
+    float* s_red = s_scale + TN;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+    const int rank_c = (int)(blockIdx.x % p.cluster), unit0 = (int)(blockIdx.x / p.cluster), n_units_grid = (int)(gridDim.x / p.cluster);
+    const int t0 = blockIdx.y * TN, nt = min(TN, p.T - t0);
+    const int b0 = rank_c * p.cta_blocks, nb = min(p.cta_blocks, p.blocks - b0);        // this CTA's blocks
+    const int wr = kWarps / p.wk;                      // row tiles of a unit
+    const int my_tile = warp / p.wk, my_k = warp % p.wk;
+    const int per_unit = nb > my_k ? (nb - my_k + p.wk - 1) / p.wk : 0;                 // this warp's blocks of a unit
+    const int units = (p.tiles + wr - 1) / wr;
+
+    // ---- the first blocks of codes are asked for before anything else
+    uint4 c0[kAhead], c1[kAhead];
+    uint32_t z0[kAhead][PB], z1[kAhead][PB];
+    auto load = [&](int slot, int unit, int i) {
+        const int tile = unit * wr + my_tile;
+        if (tile >= p.tiles) return;
+        const size_t blk = (size_t)tile * p.blocks + b0 + my_k + i * p.wk;
+        const uint8_t* c = p.codes + blk * 1024 + lane * 16;
+        c0[slot] = ld_stream16(c);
+        c1[slot] = ld_stream16(c + 512);
+        const uint8_t* z = p.sz + blk * (64 * PB) + g * (4 * PB);
+        if constexpr (PB == 1) {
+            z0[slot][0] = ld_stream4(z);
+            z1[slot][0] = ld_stream4(z + 32);
+        } else if constexpr (PB == 2) {
+            const uint2 a = __ldg(reinterpret_cast<const uint2*>(z)), b = __ldg(reinterpret_cast<const uint2*>(z + 64));
+            z0[slot][0] = a.x; z0[slot][1] = a.y; z1[slot][0] = b.x; z1[slot][1] = b.y;
+        } else {
+            const uint4 a = ld_stream16(z), b = ld_stream16(z + 128);
+            z0[slot][0] = a.x; z0[slot][1] = a.y; z0[slot][2] = a.z; z0[slot][3] = a.w;
+            z1[slot][0] = b.x; z1[slot][1] = b.y; z1[slot][2] = b.z; z1[slot][3] = b.w;
+        }
+    };
+    int lu = unit0, li = 0;                            // the next block to ask for
+    auto load_next = [&](int slot) {
+        if (lu < units && per_unit > 0) {
+            load(slot, lu, li);
+            if (++li == per_unit) { li = 0; lu += n_units_grid; }
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) load_next(j);
+
+    // ---- activations: largest magnitude per token, then operands and sums of groups
+    {
+        uint32_t* s_max = reinterpret_cast<uint32_t*>(s_scale);
+        if (tid < TN) s_max[tid] = 0u;
+        __syncthreads();
+        const int chunks = nb * 4;
+        auto raw = [&](int c, int n) -> uint4 {        // eight activations of token n: word t4 of chunk c
+            const int k = (b0 * 4 + c) * 32 + t4 * 8;
+            if (n < nt && k < p.Kd) return __ldg(reinterpret_cast<const uint4*>(p.x + (size_t)(t0 + n) * p.ldx + k));
+            return make_uint4(0, 0, 0, 0);
+        };
+        uint32_t m[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) m[j] = 0u;
+#pragma unroll 2
+        for (int c = warp; c < chunks; c += kWarps)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const uint4 v = raw(c, j * 8 + g);
+                const float f[8] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y), bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)};
+                m[j] = max(m[j], abs_max8(f));
+            }
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const uint32_t v = group_max<4>(m[j]);
+            if (t4 == 0 && v != 0u) atomicMax(&s_max[j * 8 + g], v);
+        }
+        __syncthreads();
+        float sc[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sc[j] = vector_scale(s_max[j * 8 + g]);
+        for (int c = warp * (GS / 32); c < chunks; c += kWarps * (GS / 32))
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < GS / 32; ++i) {
+                    const uint4 v = raw(c + i, j * 8 + g);
+                    const float f[8] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y), bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)};
+                    s_x[(size_t)((c + i) * NT + j) * 32 + lane] = permute8_s(f, sc[j]);
+                    sum += ((f[0] + f[1]) + (f[2] + f[3])) * sc[j] + ((f[4] + f[5]) + (f[6] + f[7])) * sc[j];
+                }
+                sum = group_sum<4>(sum);
+                if (t4 == 0) s_sum[(c / (GS / 32)) * TN + j * 8 + g] = sum * kScaleS;
+            }
+        __syncthreads();
+        if (tid < TN) s_scale[tid] = kUnscaleS * vector_unscale(vector_scale(s_max[tid]));
+        __syncthreads();
+    }
+
+    bool u_there = p.rank == 0;
+    int slot = 0;
+    for (int unit = unit0; unit < units; unit += n_units_grid) {
+        const int tile = unit * wr + my_tile;
+        float acc[NT][4];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+        // (the slots are walked by a switch over kAhead constants: registers cannot be indexed)
+        auto block = [&](int s, int i) {
+            const int lb = my_k + i * p.wk;            // block within this CTA's
+            const uint32_t w0[4] = {c0[s].x, c0[s].y, c0[s].z, c0[s].w}, w1[4] = {c1[s].x, c1[s].y, c1[s].z, c1[s].w};
+            float d[NT][4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t q0[4], q1[4];
+                dequant_word_s(w0[c], q0);
+                dequant_word_s(w1[c], q1);
+                const uint4* xb = s_x + (size_t)((lb * 4 + c) * NT) * 32 + lane;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const uint4 b = xb[j * 32];
+                    if (c % (GS / 32) == 0) mma16816_zero(d[j], q0[0], q1[0], q0[1], q1[1], b.x, b.y);
+                    else mma16816(d[j], q0[0], q1[0], q0[1], q1[1], b.x, b.y);
+                    mma16816(d[j], q0[2], q1[2], q0[3], q1[3], b.z, b.w);
+                }
+                if (c % (GS / 32) == GS / 32 - 1) {
+                    const int pi = c / (GS / 32);
+                    const float2 f0 = __half22float2(u32_as_h2(z0[s][pi])), f1 = __half22float2(u32_as_h2(z1[s][pi]));
+                    const float2* sm = reinterpret_cast<const float2*>(s_sum + (lb * PB + pi) * TN) + t4;
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        const float2 xs = sm[j * 4];
+                        acc[j][0] = fmaf(f0.x, fmaf(-f0.y, xs.x, d[j][0]), acc[j][0]);
+                        acc[j][1] = fmaf(f0.x, fmaf(-f0.y, xs.y, d[j][1]), acc[j][1]);
+                        acc[j][2] = fmaf(f1.x, fmaf(-f1.y, xs.x, d[j][2]), acc[j][2]);
+                        acc[j][3] = fmaf(f1.x, fmaf(-f1.y, xs.y, d[j][3]), acc[j][3]);
+                    }
+                }
+            }
+        };
+        for (int i = 0; i < per_unit;) {
+#pragma unroll
+            for (int s = 0; s < kAhead; ++s)
+                if (s == slot && i < per_unit) {
+                    if (tile < p.tiles) block(s, i);
+                    load_next(s);
+                    ++i;
+                    slot = s + 1 == kAhead ? 0 : s + 1;
+                }
+        }
+        // ---- partial sums meet: [warp][row][token]
+        float* red = s_red + warp * 16 * TN;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            *reinterpret_cast<float2*>(red + g * TN + j * 8 + 2 * t4) = make_float2(acc[j][0], acc[j][1]);
+            *reinterpret_cast<float2*>(red + (g + 8) * TN + j * 8 + 2 * t4) = make_float2(acc[j][2], acc[j][3]);
+        }
+        if (p.cluster > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
+        if (!u_there) { pdl_wait_prior_grid(); u_there = true; }
+        // outputs of the unit, spread over the cluster's CTAs; consecutive threads take consecutive rows of a token
+        const int outs = wr * 16 * nt;
+        for (int o = rank_c * kThreads + tid; o < outs; o += p.cluster * kThreads) {
+            const int row = o % (wr * 16), tok = o / (wr * 16), rt = row >> 4;
+            const int n = (unit * wr + rt) * 16 + (row & 15);
+            if (n >= p.N) continue;
+            float v = 0.f;
+            const float* src = s_red + rt * p.wk * 16 * TN + (row & 15) * TN + tok;
+            if (p.cluster > 1) {
+                for (int c = 0; c < p.cluster; ++c) {
+                    float part = 0.f, us;
+                    for (int k = 0; k < p.wk; ++k) {
+                        float f;
+                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(map_to_cta(src + k * 16 * TN, c)));
+                        part += f;
+                    }
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(us) : "r"(map_to_cta(s_scale + tok, c)));
+                    v = fmaf(part, us, v);
+                }
+            } else {
+                for (int k = 0; k < p.wk; ++k) v += src[k * 16 * TN];
+                v *= s_scale[tok];
+            }
+            if (p.rank > 0) {
+                const uint16_t* Bn = p.B + (size_t)n * p.rank;
+                const float* ut = p.u + (size_t)(t0 + tok) * p.rank;
+                float e = 0.f;
+                for (int r = 0; r < p.rank; ++r) e = fmaf(bf16_bits_to_float(Bn[r]), __ldcg(ut + r), e);
+                v = fmaf(p.lora_scale, e, v);
+            }
+            const size_t at = (size_t)(t0 + tok) * p.ldy + n;
+            if (p.out_dtype == EDG_F32) store_out(static_cast<float*>(p.y), at, v);
+            else if (p.out_dtype == EDG_F16) store_out(static_cast<__half*>(p.y), at, v);
+            else static_cast<uint16_t*>(p.y)[at] = bf16_rn(v);
+        }
+        __syncwarp();
+        // (the next unit's partial sums wait until these have been read)
+        if (p.cluster > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
+    }
+    if (!u_there) pdl_wait_prior_grid();
+}
+
+template <int GS, int NT> int32_t launch_linear(LinearParams& p, cudaStream_t st) {
+    static OncePerDevice once;
+    constexpr size_t kMost = 200 * 1024;
+    EDG_CUDA_TRY(once([] { return allow_smem(kMost, linear_kernel<GS, NT>); }));
+    const int sms = sm_count();
+    // row tiles that a CTA takes at a time: one, all warps on it, unless there are many more than SMs
+    p.wk = kWarps;
+    while (p.wk > 2 && p.tiles / (kWarps / p.wk) > 16 * sms) p.wk >>= 1;
+    const int units = (p.tiles + kWarps / p.wk - 1) / (kWarps / p.wk);
+    const int slices = (p.T + NT * 8 - 1) / (NT * 8);
+    // CTAs of a cluster share the input dimension: as many as shared memory asks for, and more while there are SMs without work
+    // and each keeps a block for every warp
+    p.cluster = 1;
+    auto bytes = [&](int c) { return linear_smem<GS, NT>((p.blocks + c - 1) / c); };
+    while (p.cluster < 8 && (bytes(p.cluster) > kMost || ((int64_t)units * slices * p.cluster * 2 <= sms && p.blocks >= 2 * p.cluster * kWarps)))
+        p.cluster *= 2;
+    if (bytes(p.cluster) > kMost) return EDG_E_SHAPE;
+    p.cta_blocks = (p.blocks + p.cluster - 1) / p.cluster;
+    const size_t smem = bytes(p.cluster);
+    int resident = (int)((220 * 1024) / (smem + 1024));
+    resident = resident < 1 ? 1 : (resident > kResident<NT> ? kResident<NT> : resident);
+    const int most = (sms * resident / p.cluster > 0 ? sms * resident / p.cluster : 1);
+    const int waves = (units + most - 1) / most;
+    const int grid = (units + waves - 1) / waves;
+    EDG_CUDA_TRY(p.rank > 0 ? launch_pdl_cluster(p.cluster, linear_kernel<GS, NT>, dim3(grid * p.cluster, slices), kThreads, smem, st, p)
+                            : launch_cluster(p.cluster, linear_kernel<GS, NT>, dim3(grid * p.cluster, slices), kThreads, smem, st, p));
+    return EDG_OK;
+}
+
+template <int GS> int32_t launch_gs(LinearParams& p, cudaStream_t st) {
+    // as many tokens a pass as there are, up to 64, and fewer where their activations do not fit the shared memory of eight CTAs
+    int nt = p.T <= 8 ? 1 : (p.T <= 16 ? 2 : (p.T <= 32 ? 4 : 8));
+    while (nt > 1 && (size_t)((p.blocks + 7) / 8) * nt * (2048 + 32 * (128 / GS)) + nt * 8 * 4 * 129 > 200 * 1024) nt >>= 1;
+    switch (nt) {
+        case 1: return launch_linear<GS, 1>(p, st);
+        case 2: return launch_linear<GS, 2>(p, st);
+        case 4: return launch_linear<GS, 4>(p, st);
+        default: return launch_linear<GS, 8>(p, st);
+    }
+}
+
+}  // namespace
+}  // namespace edg
+
+using namespace edg;
+
+extern "C" int32_t edg_linear_record_bytes(const edg_linear_desc* desc, size_t* bytes) {
+    const int32_t rc = check(desc);
+    if (rc != EDG_OK) return rc;
+    if (!bytes) return EDG_E_INVAL;
+    *bytes = record_size(*desc);
+    return EDG_OK;
+}
+
+extern "C" int32_t edg_pack_linear(const edg_linear_desc* desc, const uint8_t* codes, const uint16_t* scales, const uint16_t* zeros, void* record) {
+    const int32_t rc = check(desc);
+    if (rc != EDG_OK) return rc;
+    if (!codes || !scales || !zeros || !record) return EDG_E_INVAL;
+    if (!zero_points_ok(zeros, (size_t)desc->N * (desc->Kd / desc->group))) return EDG_E_RANGE;
+    memset(record, 0, record_size(*desc));
+    repack_linear(*desc, static_cast<uint8_t*>(record), const_cast<uint8_t*>(codes), const_cast<uint16_t*>(scales), const_cast<uint16_t*>(zeros), true);
+    return EDG_OK;
+}
+
+extern "C" int32_t edg_unpack_linear(const edg_linear_desc* desc, const void* record, uint8_t* codes, uint16_t* scales, uint16_t* zeros) {
+    const int32_t rc = check(desc);
+    if (rc != EDG_OK) return rc;
+    if (!codes || !scales || !zeros || !record) return EDG_E_INVAL;
+    repack_linear(*desc, static_cast<uint8_t*>(const_cast<void*>(record)), codes, scales, zeros, false);
+    return EDG_OK;
+}
+
+extern "C" int32_t edg_linear_workspace_bytes(const edg_linear_desc* desc, int32_t T, size_t* bytes) {
+    const int32_t rc = check(desc);
+    if (rc != EDG_OK) return rc;
+    if (!bytes || T < 1 || T > 65535) return EDG_E_INVAL;
+    *bytes = round_up((size_t)T * (desc->rank > 0 ? desc->rank : 1) * sizeof(float), 256);
+    return EDG_OK;
+}
+
+extern "C" int32_t linear_int4_lora(const edg_linear_desc* desc, const void* record, int32_t T, const void* x, const void* A, const void* B,
+                                    void* y, void* workspace, size_t workspace_bytes, void* stream) {
+    const int32_t rc = check(desc);
+    if (rc != EDG_OK) return rc;
+    if (!record || !x || !y || !workspace || T < 1 || T > 65535) return EDG_E_INVAL;
+    if (desc->rank > 0 && (!A || !B)) return EDG_E_INVAL;
+    const size_t out = desc->out_dtype == EDG_F32 ? 4 : 2;
+    if (!aligned(record, 256) || !aligned(x, 16) || !aligned(y, out) || (desc->rank > 0 && (!aligned(A, 16) || !aligned(B, 16)))) return EDG_E_INVAL;
+    size_t need = 0;
+    edg_linear_workspace_bytes(desc, T, &need);
+    if (!aligned(workspace, 256) || workspace_bytes < need) return EDG_E_WORKSPACE;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    LinearParams p = {};
+    p.codes = static_cast<const uint8_t*>(record);
+    p.sz = p.codes + codes_bytes(*desc);
+    p.x = static_cast<const uint16_t*>(x);
+    p.B = static_cast<const uint16_t*>(B);
+    p.y = y;
+    p.N = desc->N;
+    p.Kd = desc->Kd;
+    p.T = T;
+    p.rank = desc->rank;
+    p.out_dtype = desc->out_dtype;
+    p.ldx = desc->ldx != 0 ? desc->ldx : desc->Kd;
+    p.ldy = (size_t)(desc->ldy != 0 ? desc->ldy : desc->N);
+    p.tiles = (int)tiles_of(desc->N);
+    p.blocks = blocks_of(desc->Kd);
+    p.lora_scale = desc->lora_scale;
+    if (p.rank > 0) {
+        float* u = static_cast<float*>(workspace);
+        p.u = u;
+        linear_u_kernel<<<dim3((p.rank + 3) / 4, T), 128, 0, st>>>(static_cast<const uint16_t*>(A), p.x, u, p.Kd, p.ldx, p.rank);
+        EDG_CUDA_TRY(cudaGetLastError());
+    }
+    switch (pair_codes(desc->group)) {
+        case 32: return launch_gs<32>(p, st);
+        case 64: return launch_gs<64>(p, st);
+        default: return launch_gs<128>(p, st);
+    }
+}

@@ -60,7 +60,7 @@ static bool zero_point_ok(uint16_t bits) {
     return (man & ((1 << shift) - 1)) == 0;
 }
 
-static bool zero_points_ok(const uint16_t* z, size_t n) {
+bool zero_points_ok(const uint16_t* z, size_t n) {
     for (size_t i = 0; i < n; ++i)
         if (!zero_point_ok(z[i])) return false;
     return true;

@@ -24,9 +24,10 @@ static struct {
     __typeof__(&moe_layer_decode_dependent) moe_layer_decode_dependent;
     __typeof__(&edg_stack_decode_token) edg_stack_decode_token;
     __typeof__(&edg_next_hidden_state) edg_next_hidden_state;
+    __typeof__(&linear_int4_lora) linear_int4_lora;
 } F;
 static PyObject *py_ptr, *py_stream, *py_check;               /* binding._ptr, binding._stream, binding._check */
-static PyObject *t_desc, *t_lora, *t_int, *t_size;            /* binding.LayerDesc, binding.Lora, ctypes.c_int32, ctypes.c_size_t */
+static PyObject *t_desc, *t_lora, *t_linear, *t_int, *t_size; /* binding.LayerDesc, .Lora, .LinearDesc, ctypes.c_int32, .c_size_t */
 static PyObject *raw_stream, *raw_device;                     /* torch's current raw stream of a device, current device; or NULL */
 static PyObject *s_data_ptr, *s_is_contiguous, *s_cuda_stream, *s_value, *s_numel, *s_element_size;
 
@@ -300,9 +301,22 @@ static PyObject* py_next_hidden_state(PyObject* self, PyObject* const* a, Py_ssi
     return done(rc, "edg_next_hidden_state");
 }
 
-/* init(addresses: dict name -> int, _ptr, _stream, _check, LayerDesc, Lora, c_int32, c_size_t) */
+static PyObject* py_linear_int4_lora(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    ARGS("linear_int4_lora", 10);
+    edg_linear_desc d;
+    void *rec, *x, *A, *B, *y, *ws, *st;
+    size_t bytes;
+    int32_t T, rc;
+    if (as_struct(a[0], t_linear, &d, sizeof d, 0, NULL) || as_ptr(a[1], &rec) || as_int(a[2], &T) || as_ptr(a[3], &x) || as_ptr(a[4], &A) ||
+        as_ptr(a[5], &B) || as_ptr(a[6], &y) || as_ptr(a[7], &ws) || as_bytes(a[8], a[7], &bytes) || as_stream(a[9], &st))
+        return NULL;
+    CALL(F.linear_int4_lora(&d, rec, T, x, A, B, y, ws, bytes, st))
+    return done(rc, "linear_int4_lora");
+}
+
+/* init(addresses: dict name -> int, _ptr, _stream, _check, LayerDesc, Lora, LinearDesc, c_int32, c_size_t) */
 static PyObject* py_init(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
-    ARGS("init", 8);
+    ARGS("init", 9);
 #define TAKE(name)                                                                                        \
     do {                                                                                                  \
         PyObject* v = PyDict_GetItemString(a[0], #name);                                                  \
@@ -312,16 +326,17 @@ static PyObject* py_init(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
     } while (0)
     TAKE(prerouter_topk); TAKE(prerouter_topk_tokens); TAKE(softmax_topk_rows); TAKE(sigmoid_group_topk_rows); TAKE(prerouter_mlp_topk);
     TAKE(moe_expert_ffn_int4_lora); TAKE(moe_layer_decode); TAKE(moe_layer_decode_dependent); TAKE(edg_stack_decode_token);
-    TAKE(edg_next_hidden_state);
+    TAKE(edg_next_hidden_state); TAKE(linear_int4_lora);
     py_ptr = Py_NewRef(a[1]);
     py_stream = Py_NewRef(a[2]);
     py_check = Py_NewRef(a[3]);
-    for (int i = 4; i < 8; ++i)
+    for (int i = 4; i < 9; ++i)
         if (!PyType_Check(a[i])) return PyErr_Format(PyExc_TypeError, "init: argument %d is no type", i);
     t_desc = Py_NewRef(a[4]);
     t_lora = Py_NewRef(a[5]);
-    t_int = Py_NewRef(a[6]);
-    t_size = Py_NewRef(a[7]);
+    t_linear = Py_NewRef(a[6]);
+    t_int = Py_NewRef(a[7]);
+    t_size = Py_NewRef(a[8]);
     Py_RETURN_NONE;
 }
 
@@ -340,7 +355,7 @@ static PyMethodDef methods[] = {
     M("softmax_topk_rows", py_softmax_topk_rows), M("sigmoid_group_topk_rows", py_sigmoid_group_topk_rows),
     M("prerouter_mlp_topk", py_prerouter_mlp_topk), M("moe_expert_ffn_int4_lora", py_moe_expert_ffn), M("moe_layer_decode", py_moe_layer_decode),
     M("moe_layer_decode_dependent", py_moe_layer_decode_dependent), M("stack_decode_token", py_stack_decode_token),
-    M("next_hidden_state", py_next_hidden_state), {NULL, NULL, 0, NULL}};
+    M("next_hidden_state", py_next_hidden_state), M("linear_int4_lora", py_linear_int4_lora), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_edgcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__edgcall(void) {
