@@ -442,6 +442,123 @@ int32_t edg_linear_workspace_bytes(const edg_linear_desc* desc, int32_t T, size_
 int32_t linear_int4_lora(const edg_linear_desc* desc, const void* record, int32_t T, const void* x, const void* A, const void* B,
                          void* y, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------- pages of a cache */
+
+/* The cache of a decoder's requests in pages of `page` tokens: which pages a sequence holds and how many sequences hold a page.  All
+ * of it is device memory, and every call below works on the stream alone (no host round trip, capturable): the state is
+ * the same whether the calls are issued one by one or replayed.  A free page has 0 references; a sequence that holds nothing has
+ * length 0; the caller starts with refs and lens at zero.  Entries of the table behind a sequence's pages are not read; pages_free
+ * sets those it releases to -1. */
+typedef struct edg_page_pool {
+    int32_t  n_pages;    /* pages in the pool                                                            */
+    int32_t  page;       /* tokens to a page                                                             */
+    int32_t  n_seqs;     /* rows of the table                                                            */
+    int32_t  max_pages;  /* pages a sequence can hold                                                    */
+    int32_t* refs;       /* dev [n_pages]: sequences that hold the page                                  */
+    int32_t* table;      /* dev [n_seqs][max_pages]: page of every `page` tokens of a sequence           */
+    int32_t* lens;       /* dev [n_seqs]: tokens of a sequence                                           */
+} edg_page_pool;
+
+/* The memory behind the pages: for every layer n_pages pages of page * row_bytes bytes. */
+typedef struct edg_page_cache {
+    void*   base;          /* dev [n_layers] of n_pages pages, 16-byte aligned                           */
+    int64_t layer_stride;  /* bytes from one layer to the next, a multiple of 16                         */
+    int32_t n_layers;
+    int32_t n_pages;
+    int32_t page;          /* tokens to a page                                                           */
+    int32_t row_bytes;     /* bytes of a token, a multiple of 16                                         */
+} edg_page_cache;
+
+/* Bytes of device scratch that the calls below need.  As with the FFN's workspace the first 4096 bytes are a control block that the
+ * caller zeroes once; its status word (edg_workspace_status) is sticky: EDG_E_RANGE for an index or length outside its range or a
+ * rule below that was broken, EDG_E_SLOTS when the pool had too few free pages.  Calls that share one must be ordered on the device. */
+int32_t edg_pages_workspace_bytes(const edg_page_pool* pool, size_t* bytes);
+
+/* Each of children[i] (dev int32 [n], 1 <= n <= 1024) becomes a copy of parents[i] (dev int32 [n]) by sharing all its pages: no row is
+ * copied.  A child must be empty, must not be listed twice, and no parent of the call may be one of its children; a pair that breaks this is
+ * skipped and raises EDG_E_RANGE.  A parent may be listed any number of times. */
+int32_t edg_pages_fork(const edg_page_pool* pool, int32_t n, const int32_t* parents, const int32_t* children,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* Each of seqs[i] (dev int32 [n], 1 <= n <= 1024, distinct: a later mention is skipped and raises EDG_E_RANGE) grows by counts[i] >= 0 tokens.  A last
+ * page that is partly filled and shared is replaced by a copy of its filled rows first (in every layer of `cache`), so that what is
+ * written behind them reaches this sequence alone; of all holders that grow, the last in the list keeps the page if no
+ * other holds it.  New pages are the lowest-numbered free ones, given out in the order of the list: first the copy, then the
+ * others.  Where the pool has too few free pages for the whole list, nothing is changed and EDG_E_SLOTS is raised. */
+int32_t edg_pages_reserve(const edg_page_pool* pool, const edg_page_cache* cache, int32_t n, const int32_t* seqs, const int32_t* counts,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Each of seqs[i] (dev int32 [n], 1 <= n <= 1024; a later mention changes nothing) gives its pages back and becomes empty. */
+int32_t edg_pages_free(const edg_page_pool* pool, int32_t n, const int32_t* seqs, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Moves pages in use to the front of the pool: with u pages in use, those at u and behind move, in ascending order, to the free ones
+ * before u, in ascending order; tables and reference counts follow, rows are copied in every layer.  What the freed pages hold is left. */
+int32_t edg_pages_compact(const edg_page_pool* pool, const edg_page_cache* cache, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Page src_pages[i] of `src` is copied to page dst_pages[i] of `dst` in every layer (dev int32 [n], 1 <= n <= 65535; same page, row_bytes and
+ * n_layers; the two caches are the same memory or do not overlap).  Of several entries with one destination the last is
+ * carried out.  Within one cache an entry whose destination is the source of another entry is skipped and raises EDG_E_RANGE. */
+int32_t edg_pages_copy(const edg_page_cache* dst, const edg_page_cache* src, int32_t n, const int32_t* dst_pages, const int32_t* src_pages,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------- latent attention */
+
+/* Attention whose keys and values of all heads come from one shared latent vector a token (the attention of the paper's 8B tier;
+ * the routed experts sit behind it).  Cache row j holds c_j (d_latent, normed) and p_j (d_rope, rotated); with W_uk and W_uv per head
+ *     s_jh = scale * (q_nope . W_uk[h] c_j  +  q_rope . p_j),     y_h = sum_j softmax(s)_j W_uv[h] c_j,
+ * over the positions j up to the row's own.  Two forms of the same function:
+ *   absorbed   q_lat = W_uk[h]^T q_nope, o_lat = sum_j p_j c_j, y = W_uv[h] o_lat: reads every cache row once for all heads (decoding)
+ *   expanded   keys and values of every head are written out once, then plain attention over them (prompts)
+ * Both take bf16 operands with fp32 sums and softmax; q_lat, o_lat (as two bf16 parts) and the weights p_j enter products as bf16 in
+ * the absorbed form, the expanded keys and values in the other: half a bf16 step each, as y itself. */
+#define EDG_LATENT_AUTO     0
+#define EDG_LATENT_ABSORBED 1
+#define EDG_LATENT_EXPANDED 2
+typedef struct edg_latent_desc {
+    int32_t heads;        /* 1 to 256                                                                    */
+    int32_t d_nope;       /* part of a query and key without position: a multiple of 16, at most 128     */
+    int32_t d_rope;       /* rotated part: a multiple of 16, at most 64                                  */
+    int32_t d_v;          /* values: a multiple of 16, at most 128                                       */
+    int32_t d_latent;     /* 128, 256, 384 or 512                                                        */
+    int32_t page;         /* tokens to a page: 16, 32, 64, 128 or 256                                    */
+    int32_t n_pages;      /* pages of the cache, n_pages * page < 2^31                                   */
+    int32_t max_pages;    /* columns of the page table                                                   */
+    int32_t out_dtype;    /* type of y: EDG_F16 or EDG_BF16                                              */
+    int32_t rope_halves;  /* pairs that are rotated: 0 (2j, 2j+1), 1 (j, j + d_rope/2)                   */
+    int32_t form;         /* EDG_LATENT_AUTO, _ABSORBED or _EXPANDED (attention)                         */
+    int32_t ldkv;         /* elements between rows of kv, a multiple of 8; 0 = d_latent + d_rope         */
+    int32_t ldq;          /* elements between rows of q, a multiple of 8; 0 = heads * (d_nope + d_rope)  */
+    float   scale;        /* of the scores, usually 1 / sqrt(d_nope + d_rope)                            */
+} edg_latent_desc;
+
+/* Bytes of device scratch for calls with up to n_seqs sequences, T new rows in all, max_new of one sequence, total_len positions in
+ * all.  First 4096 bytes: control block as elsewhere (zeroed once by the caller, status word).  None of the arguments makes it fall. */
+int32_t edg_latent_workspace_bytes(const edg_latent_desc* desc, int32_t n_seqs, int32_t T, int32_t max_new, int64_t total_len, size_t* bytes);
+
+/* New rows of the cache.  Sequence i has the new rows cu[i] .. cu[i+1] - 1 (dev int32 [n_seqs + 1], cu[0] = 0, not falling; cu[n_seqs] <= T: rows
+ * behind the last sequence are not touched) and lens[i] positions in all (dev int32 [n_seqs]), the new ones last: row r of
+ * it stands at position lens[i] - new + r.  Per row t:
+ *     c = kv[t][: d_latent] / sqrt(mean of squares + eps) * gain,   p = kv[t][d_latent :] rotated by position * inv_freq
+ * written to cache [page][row] as the table (dev int32 [n_seqs][max_pages]) says; q_rope[t][h] = the rotated part of q[t][h].
+ *   kv dev bf16 [T][ldkv]; gain dev bf16 [d_latent] or NULL; inv_freq dev float [d_rope / 2]; angles are formed in double
+ *   q dev bf16 [T][ldq] = [heads][d_nope + d_rope], q_rope dev bf16 [T][heads][d_rope], or both NULL
+ *   cache dev bf16 [n_pages][page][d_latent + d_rope], 16-byte aligned like all of them
+ * A row whose position or page lies outside its range is skipped and raises EDG_E_RANGE. */
+int32_t latent_append(const edg_latent_desc* desc, int32_t n_seqs, int32_t T, const int32_t* cu, const int32_t* lens, const int32_t* table,
+                      const void* kv, const void* gain, float eps, const float* inv_freq, const void* q, void* q_rope, void* cache,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Attention of the same rows over the cache (which holds them already).  max_new and total_len bound the rows of one sequence and
+ * the sum of lens; they size the launch, the values on the device may be smaller.
+ *   q as above; q_rope dev bf16 [T][heads][d_rope] or NULL (the last d_rope of q's heads are rotated already)
+ *   W_uk dev bf16 [heads][d_nope][d_latent], W_uv dev bf16 [heads][d_v][d_latent]; y dev [T][heads][d_v] of out_dtype
+ * A new row that stands before position 0 sees nothing and gives zeros; rows behind the last sequence are not touched; what the cache
+ * holds behind a sequence's length (infinities and NaN too) does not reach y.  A sequence longer than max_pages * page, or a page outside
+ * the cache, raises EDG_E_RANGE; so does a call whose cu or lens exceed T, max_new or total_len: its results are not to be used. */
+int32_t latent_attention(const edg_latent_desc* desc, int32_t n_seqs, int32_t T, int32_t max_new, int64_t total_len, const int32_t* cu,
+                         const int32_t* lens, const int32_t* table, const void* q, const void* q_rope, const void* W_uk, const void* W_uv,
+                         const void* cache, void* y, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------- the whole layer-step */
 
 /* One layer-step of batch-1 decode (Sec. 3.2 "Motivation": the double shift).  On `stream`:

@@ -19,10 +19,13 @@ __all__ = [
     "ffn_workspace_bytes", "workspace_status", "set_trace_buffer", "prerouter_topk", "prerouter_topk_tokens", "softmax_topk_rows", "sigmoid_group_topk_rows", "prerouter_mlp_topk",
     "moe_expert_ffn_int4_lora", "moe_expert_ffn_int4_lora_static", "moe_layer_decode", "stage_experts_to_slots",
     "moe_layer_decode_dependent", "stack_decode_token", "next_hidden_state", "LinearDesc", "make_linear_desc", "linear_record_bytes", "pack_linear",
-    "unpack_linear", "linear_workspace_bytes", "linear_int4_lora", "EXPORTS",
+    "unpack_linear", "linear_workspace_bytes", "linear_int4_lora", "LatentDesc", "make_latent_desc", "latent_workspace_bytes",
+    "latent_append", "latent_attention", "LATENT_AUTO", "LATENT_ABSORBED", "LATENT_EXPANDED", "PagePool", "PageCache", "make_page_pool",
+    "make_page_cache", "pages_workspace_bytes", "pages_fork", "pages_reserve", "pages_free", "pages_compact", "pages_copy", "EXPORTS",
 ]
 
 F32, F16, BF16 = 0, 1, 2
+LATENT_AUTO, LATENT_ABSORBED, LATENT_EXPANDED = 0, 1, 2
 _ERR = {-1: "EDG_E_INVAL", -2: "EDG_E_SHAPE", -3: "EDG_E_SLOTS", -4: "EDG_E_RANGE", -5: "EDG_E_CUDA",
         -6: "EDG_E_TIMEOUT", -7: "EDG_E_WORKSPACE"}
 
@@ -54,6 +57,19 @@ class LayerDesc(C.Structure):
 
 class LinearDesc(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("N", "Kd", "group", "rank", "out_dtype", "ldx", "ldy")] + [("lora_scale", C.c_float)]
+
+
+class LatentDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("heads", "d_nope", "d_rope", "d_v", "d_latent", "page", "n_pages", "max_pages", "out_dtype", "rope_halves",
+                                          "form", "ldkv", "ldq")] + [("scale", C.c_float)]
+
+
+class PagePool(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_pages", "page", "n_seqs", "max_pages")] + [(n, C.c_void_p) for n in ("refs", "table", "lens")]
+
+
+class PageCache(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("layer_stride", C.c_int64)] + [(n, C.c_int32) for n in ("n_layers", "n_pages", "page", "row_bytes")]
 
 
 class Lora(C.Structure):
@@ -99,6 +115,8 @@ class StoreStats(C.Structure):
 _P = C.c_void_p
 _D = C.POINTER(LayerDesc)
 _DL = C.POINTER(LinearDesc)
+_DA = C.POINTER(LatentDesc)
+_PP, _PC = C.POINTER(PagePool), C.POINTER(PageCache)
 _SIG = {
     "edg_version": ([], C.c_int32),
     "edg_last_cuda_error": ([], C.c_int32),
@@ -142,6 +160,15 @@ _SIG = {
     "edg_unpack_linear": ([_DL] + [_P] * 4, C.c_int32),
     "edg_linear_workspace_bytes": ([_DL, C.c_int32, C.POINTER(C.c_size_t)], C.c_int32),
     "linear_int4_lora": ([_DL, _P, C.c_int32, _P, _P, _P, _P, _P, C.c_size_t, _P], C.c_int32),
+    "edg_pages_workspace_bytes": ([_PP, C.POINTER(C.c_size_t)], C.c_int32),
+    "edg_pages_fork": ([_PP, C.c_int32, _P, _P, _P, C.c_size_t, _P], C.c_int32),
+    "edg_pages_reserve": ([_PP, _PC, C.c_int32, _P, _P, _P, C.c_size_t, _P], C.c_int32),
+    "edg_pages_free": ([_PP, C.c_int32, _P, _P, C.c_size_t, _P], C.c_int32),
+    "edg_pages_compact": ([_PP, _PC, _P, C.c_size_t, _P], C.c_int32),
+    "edg_pages_copy": ([_PC, _PC, C.c_int32, _P, _P, _P, C.c_size_t, _P], C.c_int32),
+    "edg_latent_workspace_bytes": ([_DA, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.POINTER(C.c_size_t)], C.c_int32),
+    "latent_append": ([_DA, C.c_int32, C.c_int32, _P, _P, _P, _P, _P, C.c_float, _P, _P, _P, _P, _P, C.c_size_t, _P], C.c_int32),
+    "latent_attention": ([_DA, C.c_int32, C.c_int32, C.c_int32, C.c_int64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, C.c_size_t, _P], C.c_int32),
     "moe_layer_decode": ([_P, C.c_int32, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, C.c_size_t, _P], C.c_int32),
 }
 EXPORTS = tuple(_SIG)
@@ -187,8 +214,9 @@ def _stream(stream) -> Optional[int]:
 
 _edgcall.init({n: C.cast(getattr(_lib, n), C.c_void_p).value for n in (
     "prerouter_topk", "prerouter_topk_tokens", "softmax_topk_rows", "sigmoid_group_topk_rows", "prerouter_mlp_topk",
-    "moe_expert_ffn_int4_lora", "moe_layer_decode", "moe_layer_decode_dependent", "edg_stack_decode_token", "edg_next_hidden_state", "linear_int4_lora")},
-    _ptr, _stream, _check, LayerDesc, Lora, LinearDesc, C.c_int32, C.c_size_t)
+    "moe_expert_ffn_int4_lora", "moe_layer_decode", "moe_layer_decode_dependent", "edg_stack_decode_token", "edg_next_hidden_state", "linear_int4_lora",
+    "latent_append", "latent_attention", "edg_pages_fork", "edg_pages_reserve", "edg_pages_free", "edg_pages_compact", "edg_pages_copy")},
+    _ptr, _stream, _check, LayerDesc, Lora, LinearDesc, LatentDesc, PagePool, PageCache, C.c_int32, C.c_size_t, C.c_int64)
 
 
 _DT = {"f32": F32, "f16": F16, "bf16": BF16}
@@ -369,6 +397,70 @@ def linear_workspace_bytes(desc: LinearDesc, T: int = 1) -> int:
 def linear_int4_lora(desc, record, T, x, A, B, y, workspace, workspace_bytes=None, stream=None) -> None:
     """y[t] = W x[t] + lora_scale B (A x[t]); A and B None without an adapter."""
     _edgcall.linear_int4_lora(desc, record, T, x, A, B, y, workspace, workspace_bytes, stream)
+
+
+def make_latent_desc(*, heads, d_nope, d_rope, d_v, d_latent, page, n_pages, max_pages, scale, out_dtype="bf16", rope_halves=False,
+                     form=LATENT_AUTO, ldkv=0, ldq=0) -> LatentDesc:
+    """Descriptor of latent attention over a paged cache; ldkv / ldq: elements between rows of kv and q (0 = dense)."""
+    return LatentDesc(int(heads), int(d_nope), int(d_rope), int(d_v), int(d_latent), int(page), int(n_pages), int(max_pages),
+                      _DT[out_dtype] if isinstance(out_dtype, str) else int(out_dtype), int(rope_halves), int(form), int(ldkv), int(ldq), float(scale))
+
+
+def latent_workspace_bytes(desc: LatentDesc, n_seqs: int, T: int, max_new: int, total_len: int) -> int:
+    n = C.c_size_t()
+    _check(_lib.edg_latent_workspace_bytes(C.byref(desc), n_seqs, T, max_new, total_len, C.byref(n)), "edg_latent_workspace_bytes")
+    return n.value
+
+
+def latent_append(desc, n_seqs, T, cu, lens, table, kv, gain, eps, inv_freq, q, q_rope, cache, workspace, workspace_bytes=None, stream=None) -> None:
+    _edgcall.latent_append(desc, n_seqs, T, cu, lens, table, kv, gain, eps, inv_freq, q, q_rope, cache, workspace, workspace_bytes, stream)
+
+
+def latent_attention(desc, n_seqs, T, max_new, total_len, cu, lens, table, q, q_rope, W_uk, W_uv, cache, y, workspace, workspace_bytes=None,
+                     stream=None) -> None:
+    _edgcall.latent_attention(desc, n_seqs, T, max_new, total_len, cu, lens, table, q, q_rope, W_uk, W_uv, cache, y, workspace, workspace_bytes, stream)
+
+
+def make_page_pool(refs, table, lens, *, page) -> PagePool:
+    """The struct only carries addresses (int32 tensors refs [n_pages], table [n_seqs][max_pages], lens [n_seqs]): the caller keeps them alive."""
+    if table.shape[0] != lens.shape[0]:
+        raise ValueError("table and lens disagree about the number of sequences")
+    return PagePool(refs.shape[0], int(page), table.shape[0], table.shape[1], _ptr(refs), _ptr(table), _ptr(lens))
+
+
+def make_page_cache(cache) -> PageCache:
+    """From a tensor [layers][pages][tokens][row]; the caller keeps it alive."""
+    if cache.dim() != 4:
+        raise ValueError("a cache is [layers][pages][tokens][row]")
+    layers, pages, page, row = cache.shape
+    row_bytes = row * cache.element_size()
+    return PageCache(_ptr(cache), pages * page * row_bytes, layers, pages, page, row_bytes)
+
+
+def pages_workspace_bytes(pool: PagePool) -> int:
+    n = C.c_size_t()
+    _check(_lib.edg_pages_workspace_bytes(C.byref(pool), C.byref(n)), "edg_pages_workspace_bytes")
+    return n.value
+
+
+def pages_fork(pool, n, parents, children, workspace, workspace_bytes=None, stream=None) -> None:
+    _edgcall.pages_fork(pool, n, parents, children, workspace, workspace_bytes, stream)
+
+
+def pages_reserve(pool, cache, n, seqs, counts, workspace, workspace_bytes=None, stream=None) -> None:
+    _edgcall.pages_reserve(pool, cache, n, seqs, counts, workspace, workspace_bytes, stream)
+
+
+def pages_free(pool, n, seqs, workspace, workspace_bytes=None, stream=None) -> None:
+    _edgcall.pages_free(pool, n, seqs, workspace, workspace_bytes, stream)
+
+
+def pages_compact(pool, cache, workspace, workspace_bytes=None, stream=None) -> None:
+    _edgcall.pages_compact(pool, cache, workspace, workspace_bytes, stream)
+
+
+def pages_copy(dst, src, n, dst_pages, src_pages, workspace, workspace_bytes=None, stream=None) -> None:
+    _edgcall.pages_copy(dst, src, n, dst_pages, src_pages, workspace, workspace_bytes, stream)
 
 
 class Store:

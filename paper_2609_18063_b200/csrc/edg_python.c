@@ -25,9 +25,17 @@ static struct {
     __typeof__(&edg_stack_decode_token) edg_stack_decode_token;
     __typeof__(&edg_next_hidden_state) edg_next_hidden_state;
     __typeof__(&linear_int4_lora) linear_int4_lora;
+    __typeof__(&latent_append) latent_append;
+    __typeof__(&latent_attention) latent_attention;
+    __typeof__(&edg_pages_fork) edg_pages_fork;
+    __typeof__(&edg_pages_reserve) edg_pages_reserve;
+    __typeof__(&edg_pages_free) edg_pages_free;
+    __typeof__(&edg_pages_compact) edg_pages_compact;
+    __typeof__(&edg_pages_copy) edg_pages_copy;
 } F;
 static PyObject *py_ptr, *py_stream, *py_check;               /* binding._ptr, binding._stream, binding._check */
-static PyObject *t_desc, *t_lora, *t_linear, *t_int, *t_size; /* binding.LayerDesc, .Lora, .LinearDesc, ctypes.c_int32, .c_size_t */
+static PyObject *t_desc, *t_lora, *t_linear, *t_latent;       /* binding.LayerDesc, .Lora, .LinearDesc, .LatentDesc */
+static PyObject *t_pool, *t_cache, *t_int, *t_size, *t_long;  /* binding.PagePool, .PageCache, ctypes.c_int32, .c_size_t, .c_int64 */
 static PyObject *raw_stream, *raw_device;                     /* torch's current raw stream of a device, current device; or NULL */
 static PyObject *s_data_ptr, *s_is_contiguous, *s_cuda_stream, *s_value, *s_numel, *s_element_size;
 
@@ -104,6 +112,13 @@ static int as_int(PyObject* o, int32_t* p) {
     uint64_t v = 0;
     const int rc = as_bits(o, t_int, &v);
     *p = (int32_t)(uint32_t)v;
+    return rc;
+}
+
+static int as_long(PyObject* o, int64_t* p) {
+    uint64_t v = 0;
+    const int rc = as_bits(o, t_long, &v);
+    *p = (int64_t)v;
     return rc;
 }
 
@@ -314,9 +329,106 @@ static PyObject* py_linear_int4_lora(PyObject* self, PyObject* const* a, Py_ssiz
     return done(rc, "linear_int4_lora");
 }
 
-/* init(addresses: dict name -> int, _ptr, _stream, _check, LayerDesc, Lora, LinearDesc, c_int32, c_size_t) */
+static PyObject* py_latent_append(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    ARGS("latent_append", 16);
+    edg_latent_desc d;
+    void *cu, *lens, *table, *kv, *gain, *freq, *q, *qr, *cache, *ws, *st;
+    size_t bytes;
+    int32_t n, T, rc;
+    float eps;
+    if (as_struct(a[0], t_latent, &d, sizeof d, 0, NULL) || as_int(a[1], &n) || as_int(a[2], &T) || as_ptr(a[3], &cu) || as_ptr(a[4], &lens) ||
+        as_ptr(a[5], &table) || as_ptr(a[6], &kv) || as_ptr(a[7], &gain) || as_float(a[8], &eps) || as_ptr(a[9], &freq) || as_ptr(a[10], &q) ||
+        as_ptr(a[11], &qr) || as_ptr(a[12], &cache) || as_ptr(a[13], &ws) || as_bytes(a[14], a[13], &bytes) || as_stream(a[15], &st))
+        return NULL;
+    CALL(F.latent_append(&d, n, T, cu, lens, table, kv, gain, eps, freq, q, qr, cache, ws, bytes, st))
+    return done(rc, "latent_append");
+}
+
+static PyObject* py_latent_attention(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    ARGS("latent_attention", 17);
+    edg_latent_desc d;
+    void *cu, *lens, *table, *q, *qr, *uk, *uv, *cache, *y, *ws, *st;
+    size_t bytes;
+    int32_t n, T, most, rc;
+    int64_t total;
+    if (as_struct(a[0], t_latent, &d, sizeof d, 0, NULL) || as_int(a[1], &n) || as_int(a[2], &T) || as_int(a[3], &most) || as_long(a[4], &total) ||
+        as_ptr(a[5], &cu) || as_ptr(a[6], &lens) || as_ptr(a[7], &table) || as_ptr(a[8], &q) || as_ptr(a[9], &qr) || as_ptr(a[10], &uk) ||
+        as_ptr(a[11], &uv) || as_ptr(a[12], &cache) || as_ptr(a[13], &y) || as_ptr(a[14], &ws) || as_bytes(a[15], a[14], &bytes) || as_stream(a[16], &st))
+        return NULL;
+    CALL(F.latent_attention(&d, n, T, most, total, cu, lens, table, q, qr, uk, uv, cache, y, ws, bytes, st))
+    return done(rc, "latent_attention");
+}
+
+static PyObject* py_pages_fork(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    ARGS("pages_fork", 7);
+    edg_page_pool p;
+    void *from, *to, *ws, *st;
+    size_t bytes;
+    int32_t n, rc;
+    if (as_struct(a[0], t_pool, &p, sizeof p, 0, NULL) || as_int(a[1], &n) || as_ptr(a[2], &from) || as_ptr(a[3], &to) || as_ptr(a[4], &ws) ||
+        as_bytes(a[5], a[4], &bytes) || as_stream(a[6], &st))
+        return NULL;
+    CALL(F.edg_pages_fork(&p, n, from, to, ws, bytes, st))
+    return done(rc, "edg_pages_fork");
+}
+
+static PyObject* py_pages_reserve(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    ARGS("pages_reserve", 8);
+    edg_page_pool p;
+    edg_page_cache c;
+    void *seqs, *counts, *ws, *st;
+    size_t bytes;
+    int32_t n, rc;
+    if (as_struct(a[0], t_pool, &p, sizeof p, 0, NULL) || as_struct(a[1], t_cache, &c, sizeof c, 0, NULL) || as_int(a[2], &n) || as_ptr(a[3], &seqs) ||
+        as_ptr(a[4], &counts) || as_ptr(a[5], &ws) || as_bytes(a[6], a[5], &bytes) || as_stream(a[7], &st))
+        return NULL;
+    CALL(F.edg_pages_reserve(&p, &c, n, seqs, counts, ws, bytes, st))
+    return done(rc, "edg_pages_reserve");
+}
+
+static PyObject* py_pages_free(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    ARGS("pages_free", 6);
+    edg_page_pool p;
+    void *seqs, *ws, *st;
+    size_t bytes;
+    int32_t n, rc;
+    if (as_struct(a[0], t_pool, &p, sizeof p, 0, NULL) || as_int(a[1], &n) || as_ptr(a[2], &seqs) || as_ptr(a[3], &ws) || as_bytes(a[4], a[3], &bytes) ||
+        as_stream(a[5], &st))
+        return NULL;
+    CALL(F.edg_pages_free(&p, n, seqs, ws, bytes, st))
+    return done(rc, "edg_pages_free");
+}
+
+static PyObject* py_pages_compact(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    ARGS("pages_compact", 5);
+    edg_page_pool p;
+    edg_page_cache c;
+    void *ws, *st;
+    size_t bytes;
+    int32_t rc;
+    if (as_struct(a[0], t_pool, &p, sizeof p, 0, NULL) || as_struct(a[1], t_cache, &c, sizeof c, 0, NULL) || as_ptr(a[2], &ws) ||
+        as_bytes(a[3], a[2], &bytes) || as_stream(a[4], &st))
+        return NULL;
+    CALL(F.edg_pages_compact(&p, &c, ws, bytes, st))
+    return done(rc, "edg_pages_compact");
+}
+
+static PyObject* py_pages_copy(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    ARGS("pages_copy", 8);
+    edg_page_cache d, s;
+    void *to, *from, *ws, *st;
+    size_t bytes;
+    int32_t n, rc;
+    if (as_struct(a[0], t_cache, &d, sizeof d, 0, NULL) || as_struct(a[1], t_cache, &s, sizeof s, 0, NULL) || as_int(a[2], &n) || as_ptr(a[3], &to) ||
+        as_ptr(a[4], &from) || as_ptr(a[5], &ws) || as_bytes(a[6], a[5], &bytes) || as_stream(a[7], &st))
+        return NULL;
+    CALL(F.edg_pages_copy(&d, &s, n, to, from, ws, bytes, st))
+    return done(rc, "edg_pages_copy");
+}
+
+/* init(addresses: dict name -> int, _ptr, _stream, _check, LayerDesc, Lora, LinearDesc, LatentDesc, PagePool, PageCache, c_int32, c_size_t, c_int64) */
 static PyObject* py_init(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
-    ARGS("init", 9);
+    ARGS("init", 13);
 #define TAKE(name)                                                                                        \
     do {                                                                                                  \
         PyObject* v = PyDict_GetItemString(a[0], #name);                                                  \
@@ -327,16 +439,22 @@ static PyObject* py_init(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
     TAKE(prerouter_topk); TAKE(prerouter_topk_tokens); TAKE(softmax_topk_rows); TAKE(sigmoid_group_topk_rows); TAKE(prerouter_mlp_topk);
     TAKE(moe_expert_ffn_int4_lora); TAKE(moe_layer_decode); TAKE(moe_layer_decode_dependent); TAKE(edg_stack_decode_token);
     TAKE(edg_next_hidden_state); TAKE(linear_int4_lora);
+    TAKE(latent_append); TAKE(latent_attention);
+    TAKE(edg_pages_fork); TAKE(edg_pages_reserve); TAKE(edg_pages_free); TAKE(edg_pages_compact); TAKE(edg_pages_copy);
     py_ptr = Py_NewRef(a[1]);
     py_stream = Py_NewRef(a[2]);
     py_check = Py_NewRef(a[3]);
-    for (int i = 4; i < 9; ++i)
+    for (int i = 4; i < 13; ++i)
         if (!PyType_Check(a[i])) return PyErr_Format(PyExc_TypeError, "init: argument %d is no type", i);
     t_desc = Py_NewRef(a[4]);
     t_lora = Py_NewRef(a[5]);
     t_linear = Py_NewRef(a[6]);
-    t_int = Py_NewRef(a[7]);
-    t_size = Py_NewRef(a[8]);
+    t_latent = Py_NewRef(a[7]);
+    t_pool = Py_NewRef(a[8]);
+    t_cache = Py_NewRef(a[9]);
+    t_int = Py_NewRef(a[10]);
+    t_size = Py_NewRef(a[11]);
+    t_long = Py_NewRef(a[12]);
     Py_RETURN_NONE;
 }
 
@@ -355,7 +473,9 @@ static PyMethodDef methods[] = {
     M("softmax_topk_rows", py_softmax_topk_rows), M("sigmoid_group_topk_rows", py_sigmoid_group_topk_rows),
     M("prerouter_mlp_topk", py_prerouter_mlp_topk), M("moe_expert_ffn_int4_lora", py_moe_expert_ffn), M("moe_layer_decode", py_moe_layer_decode),
     M("moe_layer_decode_dependent", py_moe_layer_decode_dependent), M("stack_decode_token", py_stack_decode_token),
-    M("next_hidden_state", py_next_hidden_state), M("linear_int4_lora", py_linear_int4_lora), {NULL, NULL, 0, NULL}};
+    M("next_hidden_state", py_next_hidden_state), M("linear_int4_lora", py_linear_int4_lora),
+    M("latent_append", py_latent_append), M("latent_attention", py_latent_attention), M("pages_fork", py_pages_fork),
+    M("pages_reserve", py_pages_reserve), M("pages_free", py_pages_free), M("pages_compact", py_pages_compact), M("pages_copy", py_pages_copy), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_edgcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__edgcall(void) {
