@@ -32,6 +32,11 @@ struct LatentSeqs {
     int n, T, max_pages, page_shift, n_pages;
 };
 
+// The absorbed form (edg_latent_absorbed.cu): scratch, control block included, and the launches.
+size_t absorbed_workspace(const edg_latent_desc& d, int n_seqs, int T, int max_new);
+int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new, const void* q, const void* q_rope, const void* W_uk, const void* W_uv,
+                     const void* cache, void* y, void* workspace, cudaStream_t st);
+
 #ifdef __CUDACC__
 
 // Sequence of row t: the i with cu[i] <= t < cu[i + 1], or n where t lies behind the last one.  A whole warp looks: 32 places at a time.

@@ -1,0 +1,706 @@
+// Latent attention, absorbed form: queries are brought to the latent space, and every cache row is read once for all heads.
+//
+//     q_lat[t,h] = W_uk[h]^T q_nope            (absorb_kernel)
+//     s = scale (q_lat . c_j + q_rope . p_j),  O = sum_j 2^(s_j - m) c_j,  l = sum_j 2^(s_j - m)     (absorbed_kernel, over pieces of a sequence)
+//     y[t,h] = W_uv[h] (sum over pieces of O) / (sum of l)                                           (combine_kernel)
+//
+// A sequence's (row, head) pairs are the rows of one matrix product with its cache rows: 2 (2 d_l + d_r) operations a pair and
+// position against 2 (d_l + d_r) bytes a position -- 32 rows are bound by HBM, 128 by either.  absorbed_kernel gives a CTA R = 16, 32 or 64 rows
+// and streams tiles of 64 positions through shared memory by TMA.  With so few rows the second product is turned round: S = Q C^T
+// has the rows along M (64, of which R count), O^T = C^T P^T the latent dimension along M (128 at a time) and the rows along N, so that
+// O of all 512 columns takes 4 R columns of tensor memory and no lane of it idles.  C is both operands from one copy: K-major in the first
+// product, MN-major in the second.  A row of S is a thread's own: maximum and sum of the softmax need no exchange.  O is
+// rescaled only when a row's maximum has grown by more than 2^8 since it was last (p stays below 2^8, l and O are fp32).
+//
+// All positions of a batch form one line of tiles, sequence after sequence; groups of CTAs (a CTA per R rows of a sequence, side by side
+// on the same tiles, which the second then finds in L2) take equal stretches of it, whatever the lengths.  What a group has of a sequence is a piece;
+// combine_kernel adds them up in order.
+#include "edg_latent.cuh"
+#include "edg_mma.cuh"
+#include "edg_umma.cuh"
+
+namespace edg {
+
+constexpr int kGroupMost = 8;               // CTAs side by side at most; sequences of more rows come in several units
+constexpr int kSms = 148;                   // CTAs of the attention kernel: one to an SM
+
+inline int absorbed_rows(int64_t most_rows) { return most_rows <= 16 ? 16 : (most_rows <= 32 ? 32 : 64); }
+
+struct AbsorbedParams {
+    LatentSeqs s;
+    const uint16_t *q, *q_rope, *W_uk, *W_uv;
+    uint16_t* q_lat;            // [T * heads][dl + 64], the rotated part padded with zeros
+    float* part;                // [slots][group][R][dl]
+    float2* ml;                 // [slots][group][R]: maximum (in powers of two), sum
+    long long* tile_pre;        // [n + 1] tiles before a sequence
+    int32_t* unit_pre;          // [n + 1] units before it
+    void* y;
+    int32_t* status;
+    int heads, dn, dr, dv, dl, out_dtype, hr;
+    int64_t ldq, ldr;
+    float scale;
+    int R, group, groups, max_slots;
+    int max_new;
+};
+
+namespace {
+
+struct Seq { int a, rows, len, fresh, units, kt; };     // first new row, (row, head) pairs, positions, new rows, units, tiles of 64 positions
+__device__ __forceinline__ Seq sequence(const AbsorbedParams& p, int i) {
+    Seq q;
+    q.a = p.s.cu[i];
+    q.fresh = max(p.s.cu[i + 1] - q.a, 0);
+    q.len = min(max(p.s.lens[i], 0), p.s.max_pages << p.s.page_shift);
+    q.rows = q.fresh * p.heads;
+    q.units = ((q.rows + p.R - 1) / p.R + p.group - 1) / p.group;
+    q.kt = (q.len + 63) >> 6;
+    return q;
+}
+__device__ __forceinline__ long long group_start(long long W, int g, int groups) { return W * g / groups; }
+
+// ---------------------------------------------------------------- queries to the latent space
+
+// A CTA: 64 latent columns of one head, up to 64 rows.  The last CTA of the grid writes the prefix sums of tiles and units instead.
+__global__ void __launch_bounds__(128) absorb_kernel(const __grid_constant__ AbsorbedParams p) {
+    pdl_launch_dependents();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+    const int ctiles = p.dl / 64;
+    if (blockIdx.x == gridDim.x - 1) {
+        if (blockIdx.y != 0) return;
+        __shared__ long long s_t[128];
+        __shared__ int s_u[128];
+        const int per = (p.s.n + 127) / 128, i0 = min(tid * per, p.s.n), i1 = min(i0 + per, p.s.n);
+        long long t = 0;
+        int u = 0;
+        bool ok = tid != 0 || (p.s.cu[0] == 0 && p.s.cu[p.s.n] <= p.s.T);
+        for (int i = i0; i < i1; ++i) {
+            const Seq q = sequence(p, i);
+            t += (long long)q.units * q.kt;
+            u += q.units;
+            ok = ok && p.s.cu[i + 1] >= q.a && q.fresh <= p.max_new && q.len >= p.s.lens[i];
+        }
+        if (!ok) latent_raise(p.status, EDG_E_RANGE);
+        s_t[tid] = t;
+        s_u[tid] = u;
+        __syncthreads();
+        t = 0;
+        u = 0;
+        for (int j = 0; j < tid; ++j) { t += s_t[j]; u += s_u[j]; }
+        for (int i = i0; i < i1; ++i) {
+            const Seq q = sequence(p, i);
+            p.tile_pre[i] = t;
+            p.unit_pre[i] = u;
+            t += (long long)q.units * q.kt;
+            u += q.units;
+            if (i == p.s.n - 1) { p.tile_pre[p.s.n] = t; p.unit_pre[p.s.n] = u; }
+        }
+        return;
+    }
+    constexpr int kPitch = 72;                                          // elements of a row of W in shared memory: 64 and padding
+    __shared__ __align__(16) uint16_t s_w[128 * kPitch];
+    const int h = blockIdx.x / ctiles, c0 = (blockIdx.x % ctiles) * 64, row = p.dl + 64;
+    for (int i = tid; i < p.dn * 8; i += 128) {
+        const int n = i >> 3, c = (i & 7) * 8;
+        *reinterpret_cast<uint4*>(s_w + n * kPitch + c) = __ldg(reinterpret_cast<const uint4*>(p.W_uk + ((size_t)h * p.dn + n) * p.dl + c0 + c));
+    }
+    const int t_end = min(p.s.T, ((int)blockIdx.y + 1) * 64);
+    if (c0 == 0)                                                        // the rotated part, zeros behind it
+        for (int i = tid; i < (t_end - (int)blockIdx.y * 64) * 8; i += 128) {
+            const int t = blockIdx.y * 64 + (i >> 3), c = (i & 7) * 8;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (c < p.dr) v = *reinterpret_cast<const uint4*>(p.q_rope + (size_t)t * p.ldr + h * p.hr + c);
+            *reinterpret_cast<uint4*>(p.q_lat + ((size_t)t * p.heads + h) * row + p.dl + c) = v;
+        }
+    __syncthreads();
+    const int ks = p.dn / 16;
+    for (int t0 = blockIdx.y * 64; t0 < t_end; t0 += 16) {
+        float d[2][4] = {};
+        const bool r0 = t0 + g < t_end, r1 = t0 + g + 8 < t_end;
+        const uint16_t* q0 = p.q + (size_t)(t0 + g) * p.ldq + h * (p.dn + p.dr) + 2 * t4;
+        const uint16_t* q1 = q0 + 8 * p.ldq;
+#pragma unroll 4
+        for (int k = 0; k < ks; ++k) {
+            const uint32_t a0 = r0 ? *reinterpret_cast<const uint32_t*>(q0 + k * 16) : 0u, a1 = r1 ? *reinterpret_cast<const uint32_t*>(q1 + k * 16) : 0u;
+            const uint32_t a2 = r0 ? *reinterpret_cast<const uint32_t*>(q0 + k * 16 + 8) : 0u, a3 = r1 ? *reinterpret_cast<const uint32_t*>(q1 + k * 16 + 8) : 0u;
+            uint32_t b[4];                                              // k rows 0-7 and 8-15 of columns 0-7, then of columns 8-15
+            const uint32_t at = smem_u32(s_w + (k * 16 + (lane & 15)) * kPitch + warp * 16 + (lane >> 4) * 8);
+            asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]) : "r"(at));
+            mma16816_bf16(d[0], a0, a1, a2, a3, b[0], b[1]);
+            mma16816_bf16(d[1], a0, a1, a2, a3, b[2], b[3]);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int c = c0 + warp * 16 + j * 8 + 2 * t4;
+            if (r0) *reinterpret_cast<uint32_t*>(p.q_lat + ((size_t)(t0 + g) * p.heads + h) * row + c) = bf16_pair(d[j][0], d[j][1]);
+            if (r1) *reinterpret_cast<uint32_t*>(p.q_lat + ((size_t)(t0 + g + 8) * p.heads + h) * row + c) = bf16_pair(d[j][2], d[j][3]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- attention over pieces
+
+constexpr int kThreads = 256;               // warp 0 loads, warp 1 issues products, warps 4-7 softmax and epilogue
+constexpr uint32_t kUnit = 16384, kRope = 8192;      // 64 positions x 128 latent columns; x 64 rotated ones
+
+// Shared memory by R: Q [dl/64 + 1 chunks][R rows][128 bytes], P [R][128 bytes], rings of rotated parts and of units of 128 columns.
+template <int R> struct Plan {
+    static constexpr int NV = R == 64 ? 8 : (R == 32 ? 10 : 11), NR = R == 64 ? 2 : 3;
+    static constexpr uint32_t q = 0, p = 9 * R * 128, rope = p + R * 128, unit = rope + NR * kRope, bars = unit + NV * kUnit;
+    static constexpr uint32_t alpha = bars + (2 * NV + 2 * NR + 12) * 8, end = alpha + 64 * 4 + 64, bytes = end + 1024;
+    static constexpr uint32_t columns = R == 64 ? 512 : 256;            // of tensor memory: S twice 64, O 4 R
+    static_assert(bytes <= 227 * 1024, "shared memory");
+    static_assert(p % 1024 == 0 && rope % 1024 == 0 && unit % 1024 == 0, "swizzle atoms");
+};
+
+// The pieces of a CTA, one after the other; every role walks them for itself.
+struct Walk {
+    int seq, unit, ug, tile;
+    long long left;
+    Seq q;
+    // the piece
+    int row0, rows, t0, t1, slot;
+    __device__ __forceinline__ bool next(const AbsorbedParams& p, int g, int r) {
+        while (left > 0 && seq < p.s.n) {
+            q = sequence(p, seq);
+            if (ug >= q.units || q.kt == 0) { unit += q.units - ug; ++seq; ug = 0; tile = 0; continue; }
+            t0 = tile;
+            t1 = (int)min((long long)q.kt, t0 + left);
+            left -= t1 - t0;
+            slot = g + unit;
+            const int first = (ug * p.group + r) * p.R;
+            row0 = q.a * p.heads + first;
+            rows = min(q.rows - first, p.R);
+            tile = t1;
+            if (tile == q.kt) { tile = 0; ++ug; ++unit; }
+            if (rows > 0) { first_row = first; return true; }
+        }
+        return false;
+    }
+    int first_row;              // row0 within the sequence
+};
+
+template <int R>
+__global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_constant__ AbsorbedParams p, const __grid_constant__ CUtensorMap kv_map,
+                                                               const __grid_constant__ CUtensorMap q_map) {
+    using P = Plan<R>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    const uint32_t sb = smem_u32(smem);
+    uint64_t* v_full = reinterpret_cast<uint64_t*>(smem + P::bars);      // [NV]
+    uint64_t* v_empty = v_full + P::NV;
+    uint64_t* r_full = v_empty + P::NV;                                  // [NR]
+    uint64_t* r_empty = r_full + P::NR;
+    uint64_t* q_full = r_empty + P::NR;
+    uint64_t* q_empty = q_full + 1;
+    uint64_t* s_full = q_empty + 1;                                      // [2]
+    uint64_t* s_empty = s_full + 2;                                      // [2]
+    uint64_t* p_full = s_empty + 2;
+    uint64_t* pv_done = p_full + 1;
+    uint64_t* o_empty = pv_done + 1;
+    uint32_t* s_tmem = reinterpret_cast<uint32_t*>(o_empty + 1);
+    float* s_alpha = reinterpret_cast<float*>(smem + P::alpha);
+    __shared__ long long s_tiles[kThreads / 32], s_from[2];
+    __shared__ int s_units[kThreads / 32], s_at[3];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int g = blockIdx.x / p.group, r = blockIdx.x % p.group;
+    if (tid == 0) {
+        for (int i = 0; i < P::NV; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1); }
+        for (int i = 0; i < P::NR; ++i) { mbar_init(&r_full[i], 1); mbar_init(&r_empty[i], 1); }
+        mbar_init(q_full, 1);
+        mbar_init(q_empty, 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&s_empty[i], 4); }
+        mbar_init(p_full, 4);
+        mbar_init(pv_done, 1);
+        mbar_init(o_empty, 4);
+        fence_barrier_init();
+    }
+    if (warp == 1) tmem_alloc(s_tmem, P::columns);
+    if (warp == 0 && elected()) { prefetch_map(&kv_map); prefetch_map(&q_map); }
+    // ---- this group's stretch of the line of tiles, and the sequence it begins in
+    {
+        const int per = (p.s.n + kThreads - 1) / kThreads, i0 = min(tid * per, p.s.n), i1 = min(i0 + per, p.s.n);
+        long long t = 0;
+        int u = 0;
+        for (int i = i0; i < i1; ++i) {
+            const Seq q = sequence(p, i);
+            t += (long long)q.units * q.kt;
+            u += q.units;
+        }
+        long long xt = t;
+        int xu = u;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long yt = __shfl_up_sync(0xFFFFFFFFu, xt, o);
+            const int yu = __shfl_up_sync(0xFFFFFFFFu, xu, o);
+            if (lane >= o) { xt += yt; xu += yu; }
+        }
+        if (lane == 31) { s_tiles[warp] = xt; s_units[warp] = xu; }
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        long long W = 0, before = xt - t;
+        int ub = xu - u;
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w < warp) { before += s_tiles[w]; ub += s_units[w]; }
+            W += s_tiles[w];
+        }
+        const long long start = group_start(W, g, p.groups), end = group_start(W, g + 1, p.groups);
+        if (tid == 0) { s_from[1] = end - start; if (end <= start) { s_from[0] = 0; s_at[0] = s_at[1] = s_at[2] = 0; } }
+        if (end > start && t > 0 && before <= start && start < before + t) {
+            for (int i = i0; i < i1; ++i) {
+                const Seq q = sequence(p, i);
+                const long long here = (long long)q.units * q.kt;
+                if (start < before + here) {
+                    const int ug = (int)((start - before) / q.kt);
+                    s_at[0] = i;
+                    s_at[1] = ug;
+                    s_at[2] = ub + ug;
+                    s_from[0] = (start - before) % q.kt;
+                    break;
+                }
+                before += here;
+                ub += q.units;
+            }
+        }
+        __syncthreads();
+    }
+    Walk w;
+    w.seq = s_at[0];
+    w.ug = s_at[1];
+    w.unit = s_at[2];
+    w.tile = (int)s_from[0];
+    w.left = s_from[1];
+    const uint32_t tmem = *s_tmem;
+    const int NU = p.dl / 128;
+
+    if (warp == 0) {
+        // ============================================= loads: a warp walks, one lane of it issues
+        const int br = min(1 << p.s.page_shift, 64), boxes = 64 / br, outside = p.s.n_pages << p.s.page_shift;
+        RingAt v, ro;
+        uint32_t q_phase = 1;
+        bool waited = false;
+        while (w.next(p, g, r)) {
+            const int32_t* table = p.s.table + (size_t)w.seq * p.s.max_pages;
+            int base = -64, coord = 0;                                   // boxes base .. base + 31 are known, one to a lane
+            for (int t = w.t0; t < w.t1; ++t) {
+                if (t * boxes - base + boxes > 32) {
+                    base = t * boxes;
+                    const int at = (base + lane) * br;                   // first position of the lane's box
+                    coord = outside;
+                    if (at < w.q.len) {
+                        const int pg = table[at >> p.s.page_shift];
+                        if (pg >= 0 && pg < p.s.n_pages) coord = (pg << p.s.page_shift) + (at & ((1 << p.s.page_shift) - 1));
+                        else latent_raise(p.status, EDG_E_RANGE);
+                    }
+                }
+                int y[4];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) y[b] = __shfl_sync(0xFFFFFFFFu, coord, (t * boxes - base + min(b, boxes - 1)) & 31);
+                role_wait(&r_empty[ro.slot], ro.phase ^ 1, p.status);
+                if (lane == 0) {
+                    mbar_expect_tx(&r_full[ro.slot], kRope);
+                    for (int b = 0; b < boxes; ++b) tma_2d(sb + P::rope + ro.slot * kRope + b * br * 128, &kv_map, p.dl, y[b], &r_full[ro.slot]);
+                }
+                ro.next(P::NR);
+                for (int u = 0; u < NU; ++u) {
+                    role_wait(&v_empty[v.slot], v.phase ^ 1, p.status);
+                    if (lane == 0) {
+                        mbar_expect_tx(&v_full[v.slot], kUnit);
+                        for (int c = 0; c < 2; ++c)
+                            for (int b = 0; b < boxes; ++b)
+                                tma_2d(sb + P::unit + v.slot * kUnit + c * kRope + b * br * 128, &kv_map, u * 128 + c * 64, y[b], &v_full[v.slot]);
+                    }
+                    v.next(P::NV);
+                }
+                if (t == w.t0) {                                         // (behind the first tile: that does not wait for the kernel before)
+                    if (!waited) { pdl_wait_prior_grid(); waited = true; }
+                    role_wait(q_empty, q_phase, p.status);
+                    q_phase ^= 1;
+                    if (lane == 0) {
+                        mbar_expect_tx(q_full, (p.dl / 64 + 1) * R * 128);
+                        for (int c = 0; c <= p.dl / 64; ++c) tma_2d(sb + P::q + c * R * 128, &q_map, c * 64, w.row0, q_full);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+        if (!waited) pdl_wait_prior_grid();
+    } else if (warp == 1) {
+        // ============================================= products: S of a tile ahead of O of the one before
+        const uint32_t id_s = idesc_bf16(64, 64), id_o = idesc_bf16(128, R, true, false);
+        const uint32_t dq = desc_lo(sb + P::q), dp = desc_lo(sb + P::p), dv0 = desc_lo(sb + P::unit, kRope), dk0 = desc_lo(sb + P::unit), dr0 = desc_lo(sb + P::rope);
+        const uint32_t o0 = tmem + 128;
+        const int rks = p.dr / 16;
+        RingAt ks, kr, vs;                                               // units for S, rotated parts, units for O
+        int n = 0;                                                       // tiles issued
+        uint32_t q_phase = 0, o_phase = 1;
+        bool pending = false, pending_first = false;                     // O of the tile before is still to be issued
+        auto product_o = [&]() {
+            role_wait(p_full, (uint32_t)(n - 1) & 1, p.status);
+            if (pending_first) { role_wait(o_empty, o_phase, p.status); o_phase ^= 1; }
+            tc_fence_after();
+            for (int u = 0; u < NU; ++u) {
+                if (elected()) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        umma_ss(o0 + u * R, dv0 + ((vs.slot * kUnit + k * 2048) >> 4), dp + ((k * 32) >> 4), id_o, !(pending_first && k == 0));
+                    umma_done(&v_empty[vs.slot]);
+                    if (u == NU - 1) umma_done(pv_done);
+                }
+                __syncwarp();
+                vs.next(P::NV);
+            }
+        };
+        while (w.next(p, g, r)) {
+            role_wait(q_full, q_phase, p.status);
+            q_phase ^= 1;
+            for (int t = w.t0; t < w.t1; ++t) {
+                const int buf = n & 1;
+                role_wait(&s_empty[buf], ((uint32_t)(n >> 1) & 1) ^ 1, p.status);
+                role_wait(&r_full[kr.slot], kr.phase, p.status);
+                tc_fence_after();
+                const uint32_t d = tmem + buf * 64;
+                if (elected()) {
+                    for (int k = 0; k < rks; ++k)
+                        umma_ss(d, dq + (((p.dl / 64) * R * 128 + k * 32) >> 4), dr0 + ((kr.slot * kRope + k * 32) >> 4), id_s, k > 0);
+                }
+                __syncwarp();
+                for (int u = 0; u < NU; ++u) {
+                    role_wait(&v_full[ks.slot], ks.phase, p.status);
+                    tc_fence_after();
+                    if (elected()) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            umma_ss(d, dq + (((u * 2 + (k >> 2)) * R * 128 + (k & 3) * 32) >> 4),
+                                    dk0 + ((ks.slot * kUnit + (k >> 2) * kRope + (k & 3) * 32) >> 4), id_s, true);
+                        if (u == NU - 1) {
+                            umma_done(&s_full[buf]);
+                            umma_done(&r_empty[kr.slot]);
+                            if (t == w.t1 - 1) umma_done(q_empty);
+                        }
+                    }
+                    __syncwarp();
+                    ks.next(P::NV);
+                }
+                kr.next(P::NR);
+                if (pending) product_o();
+                pending = true;
+                pending_first = t == w.t0;
+                ++n;
+            }
+        }
+        if (pending) product_o();
+    } else if (warp >= 4) {
+        // ============================================= softmax, rescaling, epilogue
+        const int wq = warp & 3, row = wq * 16 + lane;                   // a product of M = 64 leaves its rows in 16 lanes of every 32
+        const bool mine = lane < 16 && row < R;
+        const uint32_t lanes = (uint32_t)(wq * 32) << 16;
+        const float k2 = p.scale * 1.4426950408889634f;
+        RingAt vt;                                                       // units of the tile at hand (to clear rows behind the end)
+        int n = 0;
+        while (w.next(p, g, r)) {
+            float m = -INFINITY, l = 0.f;
+            // positions that the row sees: up to its own
+            const int sees = mine && row < w.rows ? min(w.q.len, w.q.len - w.q.fresh + (w.first_row + row) / p.heads + 1) : 0;
+            for (int t = w.t0; t < w.t1; ++t, ++n) {
+                const int buf = n & 1;
+                role_wait(&s_full[buf], (uint32_t)(n >> 1) & 1, p.status);
+                tc_fence_after();
+                float s[64];
+                {
+                    uint32_t v[32];
+                    tmem_ld(tmem + lanes + buf * 64, v);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) s[j] = __uint_as_float(v[j]) * k2;
+                    tmem_ld(tmem + lanes + buf * 64 + 32, v);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) s[32 + j] = __uint_as_float(v[j]) * k2;
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s_empty[buf]);
+                const int seen = sees - t * 64;                          // of this tile
+                if (seen < 64) {
+#pragma unroll
+                    for (int j = 0; j < 64; ++j)
+                        if (j >= seen) s[j] = -INFINITY;
+                }
+                float mt = m;
+#pragma unroll
+                for (int j = 0; j < 64; ++j) mt = fmaxf(mt, s[j]);
+                if (!mine) mt = m;
+                const bool first = t == w.t0;
+                if (first) m = mt;
+                const bool grown = !first && (mt > m + 8.f);             // (m may be -infinity: anything is more)
+                const bool rescale = barrier_or(1, 128, grown);
+                if (n > 0) role_wait(pv_done, (uint32_t)(n - 1) & 1, p.status);       // O is complete, P has been read
+                if (rescale) {
+                    const float alpha = grown ? exp2_approx(m - mt) : 1.f;
+                    if (grown) { m = mt; l *= alpha; }
+                    if (mine) s_alpha[row] = alpha;
+                    barrier_sync(1, 128);
+                    tc_fence_after();
+                    for (int u = 0; u < NU; ++u)
+#pragma unroll
+                        for (int c = 0; c < R; c += 16) {
+                            uint32_t v[16];
+                            tmem_ld(tmem + lanes + 128 + u * R + c, v);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * s_alpha[c + j]);
+                            tmem_st(tmem + lanes + 128 + u * R + c, v);
+                        }
+                    tmem_st_wait();
+                    tc_fence_before();
+                }
+                const float mm = m == -INFINITY ? 0.f : m;
+                if (mine) {
+                    uint8_t* out = smem + P::p + row * 128;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {                        // eight positions to a 16-byte piece, under the swizzle
+                        uint32_t o[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            float a = exp2_approx(s[c * 8 + 2 * j] - mm), b = exp2_approx(s[c * 8 + 2 * j + 1] - mm);
+                            o[j] = bf16_pair(a, b);
+                            l += bf16_lo(o[j]) + bf16_hi(o[j]);          // (what the product sums)
+                        }
+                        *reinterpret_cast<uint4*>(out + ((c ^ (row & 7)) * 16)) = make_uint4(o[0], o[1], o[2], o[3]);
+                    }
+                }
+                const int held = w.q.len - t * 64;                       // positions of the tile that exist: clear the rows behind them
+                if (held < 64) {
+                    RingAt c = vt;
+                    for (int u = 0; u < NU; ++u) {
+                        role_wait(&v_full[c.slot], c.phase, p.status);
+                        uint8_t* unit = smem + P::unit + c.slot * kUnit;
+                        for (int i = held * 8 + (tid - 128); i < 512; i += 128) {
+                            *reinterpret_cast<uint4*>(unit + i * 16) = make_uint4(0, 0, 0, 0);
+                            *reinterpret_cast<uint4*>(unit + kRope + i * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        c.next(P::NV);
+                    }
+                }
+                for (int u = 0; u < NU; ++u) vt.next(P::NV);
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full);
+            }
+            // ---- the piece's sums
+            role_wait(pv_done, (uint32_t)(n - 1) & 1, p.status);
+            tc_fence_after();
+            const bool fits = w.slot < p.max_slots;
+            const size_t at = ((size_t)w.slot * p.group + r) * R;
+            if (fits && mine && row < w.rows) p.ml[at + row] = make_float2(m, l);
+            for (int u = 0; u < NU; ++u)
+#pragma unroll
+                for (int c = 0; c < R; c += 16) {
+                    uint32_t v[16];
+                    tmem_ld(tmem + lanes + 128 + u * R + c, v);
+                    if (fits)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (c + j < w.rows) p.part[(at + c + j) * p.dl + u * 128 + wq * 32 + lane] = __uint_as_float(v[j]);
+                }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(o_empty);
+        }
+    }
+    pdl_launch_dependents();
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) tmem_free(tmem, P::columns);
+}
+
+// ---------------------------------------------------------------- sums of the pieces, and out of the latent space
+
+// A CTA: one head of 16 rows.  The latent sums go into shared memory as two bf16 parts, 16 bits of them in all.
+__global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ AbsorbedParams p) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ long long s_a[16], s_b[16];
+    __shared__ int s_unit[16], s_row[16];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+    const int h = blockIdx.x, t0 = blockIdx.y * 16, pitch = p.dl * 2 + 64;
+    pdl_wait_prior_grid();
+    const long long W = p.tile_pre[p.s.n];
+    if (tid < 16) {
+        const int t = t0 + tid;
+        int row = -1;
+        if (t < p.s.T) {
+            int lo = 0, hi = p.s.n;                                      // ends cu[1..n] that are <= t
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (p.s.cu[mid + 1] <= t) lo = mid + 1; else hi = mid;
+            }
+            if (lo < p.s.n) {
+                const Seq q = sequence(p, lo);
+                const int in = (t - q.a) * p.heads + h, rt = in / p.R, ug = rt / p.group;
+                if (t >= q.a) {
+                    s_a[tid] = p.tile_pre[lo] + (long long)ug * q.kt;
+                    s_b[tid] = s_a[tid] + q.kt;
+                    s_unit[tid] = p.unit_pre[lo] + ug;
+                    row = (rt - ug * p.group) * p.R + in - rt * p.R;
+                }
+            }
+        }
+        s_row[tid] = row;
+    }
+    __syncthreads();
+    {
+        const int i = tid >> 4, c0 = (tid & 15) * 4, row = s_row[i];
+        float4 o[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        float top = -INFINITY, sum = 0.f;
+        if (row >= 0 && s_b[i] > s_a[i]) {
+            const long long a = s_a[i], b = s_b[i];
+            const int g0 = W > 0 ? (int)(((a + 1) * p.groups - 1) / W) : 0;
+            for (int gg = g0; gg < p.groups; ++gg) {
+                const long long from = group_start(W, gg, p.groups);
+                if (from >= b) break;
+                const int slot = gg + s_unit[i];
+                if (group_start(W, gg + 1, p.groups) == from || slot >= p.max_slots) continue;
+                const size_t at = (size_t)slot * p.group * p.R + row;
+                const float2 ml = p.ml[at];
+                const float m = fmaxf(top, ml.x), mm = m == -INFINITY ? 0.f : m;
+                const float fade = exp2f(top - mm), e = exp2f(ml.x - mm);
+                top = m;
+                sum = sum * fade + ml.y * e;
+                const float4* src = reinterpret_cast<const float4*>(p.part + at * p.dl + c0);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k * 64 < p.dl) {
+                        const float4 v = src[k * 16];
+                        o[k].x = o[k].x * fade + v.x * e; o[k].y = o[k].y * fade + v.y * e;
+                        o[k].z = o[k].z * fade + v.z * e; o[k].w = o[k].w * fade + v.w * e;
+                    }
+            }
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;                  // (nothing seen: zeros; NaN stays)
+        uint8_t* hi = smem + i * pitch + c0 * 2;
+        uint8_t* lo = hi + 16 * pitch;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k * 64 < p.dl) {
+                const float x = o[k].x * inv, y = o[k].y * inv, z = o[k].z * inv, u = o[k].w * inv;
+                const uint32_t h0 = bf16_pair(x, y), h1 = bf16_pair(z, u);
+                *reinterpret_cast<uint2*>(hi + k * 128) = make_uint2(h0, h1);
+                *reinterpret_cast<uint2*>(lo + k * 128) = make_uint2(bf16_pair(x - bf16_lo(h0), y - bf16_hi(h0)), bf16_pair(z - bf16_lo(h1), u - bf16_hi(h1)));
+            }
+    }
+    __syncthreads();
+    const int v0 = warp * 16;
+    if (v0 >= p.dv) return;
+    // lane t4 of a quad takes columns 8 t4 .. 8 t4 + 7 of every 32, of both operands: any order of k will do
+    float d[2][4] = {};
+    const uint16_t* w0 = p.W_uv + ((size_t)h * p.dv + v0 + g) * p.dl + t4 * 8;
+    const uint8_t* a0 = smem + g * pitch + t4 * 16;
+#pragma unroll 4
+    for (int k = 0; k < p.dl / 32; ++k) {
+        const uint4 b0 = __ldg(reinterpret_cast<const uint4*>(w0 + k * 32)), b1 = __ldg(reinterpret_cast<const uint4*>(w0 + 8 * (size_t)p.dl + k * 32));
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const uint8_t* a = a0 + part * 16 * pitch + k * 64;
+            const uint4 x = *reinterpret_cast<const uint4*>(a), z = *reinterpret_cast<const uint4*>(a + 8 * pitch);
+            mma16816_bf16(d[0], x.x, z.x, x.y, z.y, b0.x, b0.y);
+            mma16816_bf16(d[0], x.z, z.z, x.w, z.w, b0.z, b0.w);
+            mma16816_bf16(d[1], x.x, z.x, x.y, z.y, b1.x, b1.y);
+            mma16816_bf16(d[1], x.z, z.z, x.w, z.w, b1.z, b1.w);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        if (s_row[g + 8 * e] < 0) continue;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const size_t at = ((size_t)(t0 + g + 8 * e) * p.heads + h) * p.dv + v0 + j * 8 + 2 * t4;
+            const float x = d[j][2 * e], y = d[j][2 * e + 1];
+            if (p.out_dtype == EDG_F16) *reinterpret_cast<__half2*>(static_cast<__half*>(p.y) + at) = __floats2half2_rn(x, y);
+            else *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.y) + at) = bf16_pair(x, y);
+        }
+    }
+}
+
+struct AbsorbedLayout { int R, group, groups, slots; size_t tile_pre, unit_pre, q_lat, ml, part, bytes; };
+
+AbsorbedLayout absorbed_layout(const edg_latent_desc& d, int n_seqs, int T, int max_new) {
+    AbsorbedLayout L;
+    const int64_t rows = (int64_t)max_new * d.heads, all = (int64_t)T * d.heads;
+    L.R = absorbed_rows(rows);
+    const int64_t tiles = (rows + L.R - 1) / L.R;
+    L.group = (int)(tiles < kGroupMost ? tiles : kGroupMost);
+    L.groups = kSms / L.group;
+    // units: every sequence with rows has one and a part of one more at most
+    const int64_t with = n_seqs < T ? n_seqs : T;
+    L.slots = (int)(L.groups + with + all / ((int64_t)L.R * L.group) + 1);
+    const size_t rows_all = (size_t)kSms * L.R + (size_t)(with + 1) * L.R * L.group + (size_t)all;
+    L.tile_pre = kCtrlBytes;
+    L.unit_pre = round_up(L.tile_pre + ((size_t)n_seqs + 1) * 8, 256);
+    L.q_lat = round_up(L.unit_pre + ((size_t)n_seqs + 1) * 4, 256);
+    L.ml = round_up(L.q_lat + (size_t)all * (d.d_latent + 64) * 2, 256);
+    L.part = round_up(L.ml + rows_all * 8, 256);
+    L.bytes = round_up(L.part + rows_all * d.d_latent * 4, 256);
+    return L;
+}
+
+}  // namespace
+
+size_t absorbed_workspace(const edg_latent_desc& d, int n_seqs, int T, int max_new) { return absorbed_layout(d, n_seqs, T, max_new).bytes; }
+
+int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new, const void* q, const void* q_rope, const void* W_uk, const void* W_uv,
+                     const void* cache, void* y, void* workspace, cudaStream_t st) {
+    const AbsorbedLayout L = absorbed_layout(d, s.n, s.T, max_new);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    AbsorbedParams p = {};
+    p.s = s;
+    p.q = static_cast<const uint16_t*>(q);
+    p.ldq = latent_ldq(d);
+    p.q_rope = q_rope != nullptr ? static_cast<const uint16_t*>(q_rope) : p.q + d.d_nope;
+    p.ldr = q_rope != nullptr ? (int64_t)d.heads * d.d_rope : p.ldq;
+    p.hr = q_rope != nullptr ? d.d_rope : d.d_nope + d.d_rope;
+    p.W_uk = static_cast<const uint16_t*>(W_uk);
+    p.W_uv = static_cast<const uint16_t*>(W_uv);
+    p.q_lat = reinterpret_cast<uint16_t*>(ws + L.q_lat);
+    p.part = reinterpret_cast<float*>(ws + L.part);
+    p.ml = reinterpret_cast<float2*>(ws + L.ml);
+    p.tile_pre = reinterpret_cast<long long*>(ws + L.tile_pre);
+    p.unit_pre = reinterpret_cast<int32_t*>(ws + L.unit_pre);
+    p.y = y;
+    p.status = static_cast<int32_t*>(workspace);
+    p.heads = d.heads;
+    p.dn = d.d_nope;
+    p.dr = d.d_rope;
+    p.dv = d.d_v;
+    p.dl = d.d_latent;
+    p.out_dtype = d.out_dtype;
+    p.scale = d.scale;
+    p.R = L.R;
+    p.group = L.group;
+    p.groups = L.groups;
+    p.max_slots = L.slots;
+    p.max_new = max_new;
+    static OncePerDevice once;
+    EDG_CUDA_TRY(once([] {
+        cudaError_t e = allow_smem(Plan<16>::bytes, absorbed_kernel<16>);
+        if (e == cudaSuccess) e = allow_smem(Plan<32>::bytes, absorbed_kernel<32>);
+        if (e == cudaSuccess) e = allow_smem(Plan<64>::bytes, absorbed_kernel<64>);
+        return e;
+    }));
+    CUtensorMap kv_map, q_map;
+    const uint64_t row = (uint64_t)latent_row(d), q_row = (uint64_t)d.d_latent + 64;
+    const uint64_t kv_dims[2] = {row, (uint64_t)d.n_pages * d.page}, q_dims[2] = {q_row, (uint64_t)s.T * d.heads};
+    const uint32_t kv_box[2] = {64, (uint32_t)(d.page < 64 ? d.page : 64)}, q_box[2] = {64, (uint32_t)L.R};
+    EDG_CUDA_TRY(make_map(&kv_map, cache, 2, kv_dims, &row, kv_box));
+    EDG_CUDA_TRY(make_map(&q_map, p.q_lat, 2, q_dims, &q_row, q_box));
+    absorb_kernel<<<dim3(d.heads * (d.d_latent / 64) + 1, (s.T + 63) / 64), 128, 0, st>>>(p);
+    EDG_CUDA_TRY(cudaGetLastError());
+    const dim3 grid(L.groups * L.group);
+    EDG_CUDA_TRY(L.R == 16   ? launch_pdl(absorbed_kernel<16>, grid, kThreads, Plan<16>::bytes, st, p, kv_map, q_map)
+                 : L.R == 32 ? launch_pdl(absorbed_kernel<32>, grid, kThreads, Plan<32>::bytes, st, p, kv_map, q_map)
+                             : launch_pdl(absorbed_kernel<64>, grid, kThreads, Plan<64>::bytes, st, p, kv_map, q_map));
+    EDG_CUDA_TRY(launch_pdl(combine_kernel, dim3(d.heads, (s.T + 15) / 16), 256, (size_t)32 * (d.d_latent * 2 + 64), st, p));
+    return EDG_OK;
+}
+
+}  // namespace edg

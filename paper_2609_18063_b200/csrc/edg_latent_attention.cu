@@ -120,7 +120,7 @@ extern "C" int32_t edg_latent_workspace_bytes(const edg_latent_desc* desc, int32
     const int32_t rc = check_latent(desc);
     if (rc != EDG_OK) return rc;
     if (!bytes || n_seqs < 1 || n_seqs > 65535 || T < 1 || max_new < 1 || total_len < 0) return EDG_E_INVAL;
-    *bytes = kCtrlBytes;
+    *bytes = absorbed_workspace(*desc, n_seqs, T, max_new);
     return EDG_OK;
 }
 
@@ -138,6 +138,11 @@ extern "C" int32_t latent_attention(const edg_latent_desc* desc, int32_t n_seqs,
     size_t need = 0;
     edg_latent_workspace_bytes(desc, n_seqs, T, max_new, total_len, &need);
     if (!aligned(workspace, 256) || workspace_bytes < need) return EDG_E_WORKSPACE;
+    const bool absorbed = desc->form == EDG_LATENT_ABSORBED || (desc->form == EDG_LATENT_AUTO && max_new <= 128);
+    if (absorbed) {
+        const LatentSeqs s = {cu, lens, table, n_seqs, T, desc->max_pages, __builtin_ctz((unsigned)desc->page), desc->n_pages};
+        return run_absorbed(*desc, s, max_new, q, q_rope, W_uk, W_uv, cache, y, workspace, static_cast<cudaStream_t>(stream));
+    }
     AttendParams p = {};
     p.s = {cu, lens, table, n_seqs, T, desc->max_pages, __builtin_ctz((unsigned)desc->page), desc->n_pages};
     p.q = static_cast<const uint16_t*>(q);
