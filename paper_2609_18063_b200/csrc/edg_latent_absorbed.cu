@@ -56,7 +56,8 @@ __device__ __forceinline__ Seq sequence(const AbsorbedParams& p, int i) {
     q.kt = (q.len + 63) >> 6;
     return q;
 }
-__device__ __forceinline__ long long group_start(long long W, int g, int groups) { return W * g / groups; }
+// tiles that a group takes of a line of W
+__device__ __forceinline__ long long stretch(long long W, int groups) { return (W + groups - 1) / groups; }
 
 // ---------------------------------------------------------------- queries to the latent space
 
@@ -99,9 +100,16 @@ __global__ void __launch_bounds__(128) absorb_kernel(const __grid_constant__ Abs
     constexpr int kPitch = 72;                                          // elements of a row of W in shared memory: 64 and padding
     __shared__ __align__(16) uint16_t s_w[128 * kPitch];
     const int h = blockIdx.x / ctiles, c0 = (blockIdx.x % ctiles) * 64, row = p.dl + 64;
-    for (int i = tid; i < p.dn * 8; i += 128) {
-        const int n = i >> 3, c = (i & 7) * 8;
-        *reinterpret_cast<uint4*>(s_w + n * kPitch + c) = __ldg(reinterpret_cast<const uint4*>(p.W_uk + ((size_t)h * p.dn + n) * p.dl + c0 + c));
+    {
+        uint4 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int n = k * 16 + (tid >> 3), c = (tid & 7) * 8;
+            if (n < p.dn) v[k] = __ldg(reinterpret_cast<const uint4*>(p.W_uk + ((size_t)h * p.dn + n) * p.dl + c0 + c));
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k * 16 < p.dn) *reinterpret_cast<uint4*>(s_w + (k * 16 + (tid >> 3)) * kPitch + (tid & 7) * 8) = v[k];
     }
     const int t_end = min(p.s.T, ((int)blockIdx.y + 1) * 64);
     if (c0 == 0)                                                        // the rotated part, zeros behind it
@@ -244,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
             if (w < warp) { before += s_tiles[w]; ub += s_units[w]; }
             W += s_tiles[w];
         }
-        const long long start = group_start(W, g, p.groups), end = group_start(W, g + 1, p.groups);
+        const long long each = stretch(W, p.groups), start = min(each * g, W), end = min(start + each, W);
         if (tid == 0) { s_from[1] = end - start; if (end <= start) { s_from[0] = 0; s_at[0] = s_at[1] = s_at[2] = 0; } }
         if (end > start && t > 0 && before <= start && start < before + t) {
             for (int i = i0; i < i1; ++i) {
@@ -326,118 +334,144 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
         }
         if (!waited) pdl_wait_prior_grid();
     } else if (warp == 1) {
-        // ============================================= products: S of a tile ahead of O of the one before
-        const uint32_t id_s = idesc_bf16(64, 64), id_o = idesc_bf16(128, R, true, false);
-        const uint32_t dq = desc_lo(sb + P::q), dp = desc_lo(sb + P::p), dv0 = desc_lo(sb + P::unit, kRope), dk0 = desc_lo(sb + P::unit), dr0 = desc_lo(sb + P::rope);
-        const uint32_t o0 = tmem + 128;
+        // ============================================= S of every tile.  All that it needs is waited for before the first of its products:
+        // a wait between two of them costs as much as four of them.  (And O is another warp's, whose waits these products cover.)
+        const uint32_t id_s = idesc_bf16(64, 64);
+        const uint32_t dq = desc_lo(sb + P::q), dk0 = desc_lo(sb + P::unit), dr0 = desc_lo(sb + P::rope);
         const int rks = p.dr / 16;
-        RingAt ks, kr, vs;                                               // units for S, rotated parts, units for O
+        RingAt ks, kr;
         int n = 0;                                                       // tiles issued
-        uint32_t q_phase = 0, o_phase = 1;
-        bool pending = false, pending_first = false;                     // O of the tile before is still to be issued
-        auto product_o = [&]() {
-            role_wait(p_full, (uint32_t)(n - 1) & 1, p.status);
-            if (pending_first) { role_wait(o_empty, o_phase, p.status); o_phase ^= 1; }
-            tc_fence_after();
-            for (int u = 0; u < NU; ++u) {
-                if (elected()) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        umma_ss(o0 + u * R, dv0 + ((vs.slot * kUnit + k * 2048) >> 4), dp + ((k * 32) >> 4), id_o, !(pending_first && k == 0));
-                    umma_done(&v_empty[vs.slot]);
-                    if (u == NU - 1) umma_done(pv_done);
-                }
-                __syncwarp();
-                vs.next(P::NV);
-            }
-        };
+        uint32_t q_phase = 0;
         while (w.next(p, g, r)) {
             role_wait(q_full, q_phase, p.status);
             q_phase ^= 1;
-            for (int t = w.t0; t < w.t1; ++t) {
+            for (int t = w.t0; t < w.t1; ++t, ++n) {
                 const int buf = n & 1;
                 role_wait(&s_empty[buf], ((uint32_t)(n >> 1) & 1) ^ 1, p.status);
                 role_wait(&r_full[kr.slot], kr.phase, p.status);
+                uint32_t at[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (u < NU) {
+                        role_wait(&v_full[ks.slot], ks.phase, p.status);
+                        at[u] = dk0 + ((ks.slot * kUnit) >> 4);
+                        ks.next(P::NV);
+                    }
                 tc_fence_after();
-                const uint32_t d = tmem + buf * 64;
+                const uint32_t d = tmem + buf * 64, dr = dr0 + ((kr.slot * kRope) >> 4);
                 if (elected()) {
-                    for (int k = 0; k < rks; ++k)
-                        umma_ss(d, dq + (((p.dl / 64) * R * 128 + k * 32) >> 4), dr0 + ((kr.slot * kRope + k * 32) >> 4), id_s, k > 0);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (u < NU)
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                umma_ss(d, dq + (((u * 2 + (k >> 2)) * R * 128 + (k & 3) * 32) >> 4), at[u] + (((k >> 2) * kRope + (k & 3) * 32) >> 4), id_s, u + k > 0);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k < rks) umma_ss(d, dq + ((NU * 2 * R * 128 + k * 32) >> 4), dr + ((k * 32) >> 4), id_s, true);
+                    umma_done(&s_full[buf]);
+                    umma_done(&r_empty[kr.slot]);
+                    if (t == w.t1 - 1) umma_done(q_empty);
                 }
                 __syncwarp();
-                for (int u = 0; u < NU; ++u) {
-                    role_wait(&v_full[ks.slot], ks.phase, p.status);
-                    tc_fence_after();
-                    if (elected()) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            umma_ss(d, dq + (((u * 2 + (k >> 2)) * R * 128 + (k & 3) * 32) >> 4),
-                                    dk0 + ((ks.slot * kUnit + (k >> 2) * kRope + (k & 3) * 32) >> 4), id_s, true);
-                        if (u == NU - 1) {
-                            umma_done(&s_full[buf]);
-                            umma_done(&r_empty[kr.slot]);
-                            if (t == w.t1 - 1) umma_done(q_empty);
-                        }
-                    }
-                    __syncwarp();
-                    ks.next(P::NV);
-                }
                 kr.next(P::NR);
-                if (pending) product_o();
-                pending = true;
-                pending_first = t == w.t0;
-                ++n;
             }
         }
-        if (pending) product_o();
+    } else if (warp == 2) {
+        // ============================================= O += C^T P^T of every tile
+        const uint32_t id_o = idesc_bf16(128, R, true, false);
+        const uint32_t dp = desc_lo(sb + P::p), dv0 = desc_lo(sb + P::unit, kRope), o0 = tmem + 128;
+        RingAt vs;
+        int n = 0;
+        uint32_t o_phase = 1;
+        while (w.next(p, g, r)) {
+            role_wait(o_empty, o_phase, p.status);
+            o_phase ^= 1;
+            for (int t = w.t0; t < w.t1; ++t, ++n) {
+                role_wait(p_full, (uint32_t)n & 1, p.status);            // (whose writers have seen S: the units are there)
+                tc_fence_after();
+                RingAt at[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (u < NU) { at[u] = vs; vs.next(P::NV); }
+                const bool more = t > w.t0;
+                if (elected()) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (u < NU) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                umma_ss(o0 + u * R, dv0 + ((at[u].slot * kUnit + k * 2048) >> 4), dp + ((k * 32) >> 4), id_o, more || k > 0);
+                            umma_done(&v_empty[at[u].slot]);
+                        }
+                    umma_done(pv_done);
+                }
+                __syncwarp();
+            }
+        }
     } else if (warp >= 4) {
         // ============================================= softmax, rescaling, epilogue
-        const int wq = warp & 3, row = wq * 16 + lane;                   // a product of M = 64 leaves its rows in 16 lanes of every 32
-        const bool mine = lane < 16 && row < R;
+        // A product of M = 64 leaves its rows in 16 lanes of every 32; a load of that shape gives a lane two rows (gq, gq + 8 of the warp's
+        // 16), and of them the columns 8 j + 2 cq and the next.
+        const int wq = warp & 3, gq = lane >> 2, cq = lane & 3;
+        const bool mine = wq * 16 < R;
         const uint32_t lanes = (uint32_t)(wq * 32) << 16;
         const float k2 = p.scale * 1.4426950408889634f;
         RingAt vt;                                                       // units of the tile at hand (to clear rows behind the end)
         int n = 0;
         while (w.next(p, g, r)) {
-            float m = -INFINITY, l = 0.f;
-            // positions that the row sees: up to its own
-            const int sees = mine && row < w.rows ? min(w.q.len, w.q.len - w.q.fresh + (w.first_row + row) / p.heads + 1) : 0;
+            float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};      // (l: this lane's share)
+            int sees[2];                                                 // positions that a row sees: up to its own
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = wq * 16 + gq + 8 * i;
+                sees[i] = mine && row < w.rows ? min(w.q.len, w.q.len - w.q.fresh + (w.first_row + row) / p.heads + 1) : 0;
+            }
             for (int t = w.t0; t < w.t1; ++t, ++n) {
                 const int buf = n & 1;
                 role_wait(&s_full[buf], (uint32_t)(n >> 1) & 1, p.status);
                 tc_fence_after();
-                float s[64];
-                {
+                const bool first = t == w.t0;
+                float s[2][16], mt[2] = {m[0], m[1]};
+                if (mine) {
                     uint32_t v[32];
-                    tmem_ld(tmem + lanes + buf * 64, v);
+                    tmem_ld_rows16(tmem + lanes + buf * 64, v);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) s[j] = __uint_as_float(v[j]) * k2;
-                    tmem_ld(tmem + lanes + buf * 64 + 32, v);
+                    for (int i = 0; i < 2; ++i) {
+                        const int seen = sees[i] - t * 64 - 2 * cq;
+                        float a = -INFINITY, b = -INFINITY;
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) s[32 + j] = __uint_as_float(v[j]) * k2;
+                        for (int j = 0; j < 8; ++j) {
+                            s[i][2 * j] = __uint_as_float(v[4 * j + 2 * i]) * k2;
+                            s[i][2 * j + 1] = __uint_as_float(v[4 * j + 2 * i + 1]) * k2;
+                        }
+                        if (seen < 58) {                                 // (the last two of the lane's columns are 56 and 57 from its first)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                if (8 * j >= seen) s[i][2 * j] = -INFINITY;
+                                if (8 * j + 1 >= seen) s[i][2 * j + 1] = -INFINITY;
+                            }
+                        }
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) { a = fmaxf(a, s[i][2 * j]); b = fmaxf(b, s[i][2 * j + 1]); }
+                        a = fmaxf(a, b);
+                        a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
+                        a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
+                        mt[i] = fmaxf(mt[i], a);
+                    }
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&s_empty[buf]);
-                const int seen = sees - t * 64;                          // of this tile
-                if (seen < 64) {
-#pragma unroll
-                    for (int j = 0; j < 64; ++j)
-                        if (j >= seen) s[j] = -INFINITY;
-                }
-                float mt = m;
-#pragma unroll
-                for (int j = 0; j < 64; ++j) mt = fmaxf(mt, s[j]);
-                if (!mine) mt = m;
-                const bool first = t == w.t0;
-                if (first) m = mt;
-                const bool grown = !first && (mt > m + 8.f);             // (m may be -infinity: anything is more)
-                const bool rescale = barrier_or(1, 128, grown);
+                if (first) { m[0] = mt[0]; m[1] = mt[1]; }
+                const bool grown0 = mt[0] > m[0] + 8.f, grown1 = mt[1] > m[1] + 8.f;      // (-infinity: anything is more)
+                const bool rescale = barrier_or(1, 128, grown0 || grown1);
                 if (n > 0) role_wait(pv_done, (uint32_t)(n - 1) & 1, p.status);       // O is complete, P has been read
                 if (rescale) {
-                    const float alpha = grown ? exp2_approx(m - mt) : 1.f;
-                    if (grown) { m = mt; l *= alpha; }
-                    if (mine) s_alpha[row] = alpha;
+                    const float a0 = grown0 ? exp2_approx(m[0] - mt[0]) : 1.f, a1 = grown1 ? exp2_approx(m[1] - mt[1]) : 1.f;
+                    if (grown0) { m[0] = mt[0]; l[0] *= a0; }
+                    if (grown1) { m[1] = mt[1]; l[1] *= a1; }
+                    if (mine && cq == 0) { s_alpha[wq * 16 + gq] = a0; s_alpha[wq * 16 + gq + 8] = a1; }
                     barrier_sync(1, 128);
                     tc_fence_after();
                     for (int u = 0; u < NU; ++u)
@@ -452,19 +486,21 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                     tmem_st_wait();
                     tc_fence_before();
                 }
-                const float mm = m == -INFINITY ? 0.f : m;
                 if (mine) {
-                    uint8_t* out = smem + P::p + row * 128;
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {                        // eight positions to a 16-byte piece, under the swizzle
-                        uint32_t o[4];
+                    for (int i = 0; i < 2; ++i) {
+                        const float mm = m[i] == -INFINITY ? 0.f : m[i];
+                        const int row = wq * 16 + gq + 8 * i;
+                        uint8_t* out = smem + P::p + row * 128 + cq * 4;
+                        float la = 0.f, lb = 0.f;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            float a = exp2_approx(s[c * 8 + 2 * j] - mm), b = exp2_approx(s[c * 8 + 2 * j + 1] - mm);
-                            o[j] = bf16_pair(a, b);
-                            l += bf16_lo(o[j]) + bf16_hi(o[j]);          // (what the product sums)
+                        for (int j = 0; j < 8; ++j) {                    // two positions to a word, under the swizzle
+                            const uint32_t o = bf16_pair(exp2_approx(s[i][2 * j] - mm), exp2_approx(s[i][2 * j + 1] - mm));
+                            la += bf16_lo(o);                            // (what the product sums)
+                            lb += bf16_hi(o);
+                            *reinterpret_cast<uint32_t*>(out + ((j ^ (row & 7)) * 16)) = o;
                         }
-                        *reinterpret_cast<uint4*>(out + ((c ^ (row & 7)) * 16)) = make_uint4(o[0], o[1], o[2], o[3]);
+                        l[i] += la + lb;
                     }
                 }
                 const int held = w.q.len - t * 64;                       // positions of the tile that exist: clear the rows behind them
@@ -490,7 +526,12 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
             tc_fence_after();
             const bool fits = w.slot < p.max_slots;
             const size_t at = ((size_t)w.slot * p.group + r) * R;
-            if (fits && mine && row < w.rows) p.ml[at + row] = make_float2(m, l);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float sum = group_sum<4>(l[i]);
+                const int row = wq * 16 + gq + 8 * i;
+                if (fits && cq == 0 && mine && row < w.rows) p.ml[at + row] = make_float2(m[i], sum);
+            }
             for (int u = 0; u < NU; ++u)
 #pragma unroll
                 for (int c = 0; c < R; c += 16) {
@@ -518,15 +559,16 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
 // A CTA: one head of 16 rows.  The latent sums go into shared memory as two bf16 parts, 16 bits of them in all.
 __global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ AbsorbedParams p) {
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ long long s_a[16], s_b[16];
-    __shared__ int s_unit[16], s_row[16];
+    __shared__ int s_first[16], s_count[16], s_row[16];      // first slot, pieces, row of a slot
+    __shared__ float s_weight[16][kSms];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
     const int h = blockIdx.x, t0 = blockIdx.y * 16, pitch = p.dl * 2 + 64;
+    for (int i = tid; i < p.dv * p.dl / 64; i += 256)        // (this head's part of W_uv comes into L2 while the pieces are being made)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(p.W_uv + (size_t)h * p.dv * p.dl + (size_t)i * 64));
     pdl_wait_prior_grid();
-    const long long W = p.tile_pre[p.s.n];
     if (tid < 16) {
         const int t = t0 + tid;
-        int row = -1;
+        int row = -1, first = 0, count = 0;
         if (t < p.s.T) {
             int lo = 0, hi = p.s.n;                                      // ends cu[1..n] that are <= t
             while (lo < hi) {
@@ -537,45 +579,55 @@ __global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ Ab
                 const Seq q = sequence(p, lo);
                 const int in = (t - q.a) * p.heads + h, rt = in / p.R, ug = rt / p.group;
                 if (t >= q.a) {
-                    s_a[tid] = p.tile_pre[lo] + (long long)ug * q.kt;
-                    s_b[tid] = s_a[tid] + q.kt;
-                    s_unit[tid] = p.unit_pre[lo] + ug;
                     row = (rt - ug * p.group) * p.R + in - rt * p.R;
+                    if (q.kt > 0) {
+                        const long long each = stretch(p.tile_pre[p.s.n], p.groups), a = p.tile_pre[lo] + (long long)ug * q.kt;
+                        const int g0 = (int)(a / each), g1 = (int)((a + q.kt - 1) / each);
+                        first = g0 + p.unit_pre[lo] + ug;
+                        count = max(min(g1 - g0 + 1, p.max_slots - first), 0);
+                    }
                 }
             }
         }
         s_row[tid] = row;
+        s_first[tid] = first;
+        s_count[tid] = count;
     }
     __syncthreads();
     {
-        const int i = tid >> 4, c0 = (tid & 15) * 4, row = s_row[i];
+        const int i = tid >> 4, k0 = tid & 15, c0 = k0 * 4, row = s_row[i], count = s_count[i];
+        const size_t step = (size_t)p.group * p.R, at = (size_t)s_first[i] * step + row;
+        // weights of the pieces: 2^(m - largest m)
+        float top = -INFINITY;
+        for (int k = k0; k < count; k += 16) {
+            const float v = p.ml[at + k * step].x;
+            s_weight[i][k] = v;
+            top = fmaxf(top, v);
+        }
+#pragma unroll
+        for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+        const float mm = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+        for (int k = k0; k < count; k += 16) {
+            const float e = exp2f(s_weight[i][k] - mm);
+            s_weight[i][k] = e;
+            sum = fmaf(p.ml[at + k * step].y, e, sum);
+        }
+        sum = group_sum<16>(sum);
+        __syncwarp();
         float4 o[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        float top = -INFINITY, sum = 0.f;
-        if (row >= 0 && s_b[i] > s_a[i]) {
-            const long long a = s_a[i], b = s_b[i];
-            const int g0 = W > 0 ? (int)(((a + 1) * p.groups - 1) / W) : 0;
-            for (int gg = g0; gg < p.groups; ++gg) {
-                const long long from = group_start(W, gg, p.groups);
-                if (from >= b) break;
-                const int slot = gg + s_unit[i];
-                if (group_start(W, gg + 1, p.groups) == from || slot >= p.max_slots) continue;
-                const size_t at = (size_t)slot * p.group * p.R + row;
-                const float2 ml = p.ml[at];
-                const float m = fmaxf(top, ml.x), mm = m == -INFINITY ? 0.f : m;
-                const float fade = exp2f(top - mm), e = exp2f(ml.x - mm);
-                top = m;
-                sum = sum * fade + ml.y * e;
-                const float4* src = reinterpret_cast<const float4*>(p.part + at * p.dl + c0);
+#pragma unroll 2
+        for (int j = 0; j < count; ++j) {
+            const float e = s_weight[i][j];
+            const float4* src = reinterpret_cast<const float4*>(p.part + (at + j * step) * p.dl + c0);
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (k * 64 < p.dl) {
-                        const float4 v = src[k * 16];
-                        o[k].x = o[k].x * fade + v.x * e; o[k].y = o[k].y * fade + v.y * e;
-                        o[k].z = o[k].z * fade + v.z * e; o[k].w = o[k].w * fade + v.w * e;
-                    }
-            }
+            for (int k = 0; k < 8; ++k)
+                if (k * 64 < p.dl) {
+                    const float4 v = __ldcs(src + k * 16);
+                    o[k].x = fmaf(v.x, e, o[k].x); o[k].y = fmaf(v.y, e, o[k].y); o[k].z = fmaf(v.z, e, o[k].z); o[k].w = fmaf(v.w, e, o[k].w);
+                }
         }
         const float inv = sum == 0.f ? 0.f : 1.f / sum;                  // (nothing seen: zeros; NaN stays)
         uint8_t* hi = smem + i * pitch + c0 * 2;
