@@ -147,14 +147,16 @@ __global__ void __launch_bounds__(128) absorb_kernel(const __grid_constant__ Abs
 
 // ---------------------------------------------------------------- attention over pieces
 
-constexpr int kThreads = 256;               // warp 0 loads, warp 1 issues products, warps 4-7 softmax and epilogue
+constexpr int kThreads = 256;               // warps 0 and 3 load, 1 and 2 issue products, 4-7 softmax and epilogue
 constexpr uint32_t kUnit = 16384, kRope = 8192;      // 64 positions x 128 latent columns; x 64 rotated ones
+
+constexpr int kFull = 4;                    // "tile is there" barriers: more than tiles that fit the ring of rotated parts
 
 // Shared memory by R: Q [dl/64 + 1 chunks][R rows][128 bytes], P [R][128 bytes], rings of rotated parts and of units of 128 columns.
 template <int R> struct Plan {
     static constexpr int NV = R == 64 ? 8 : (R == 32 ? 10 : 11), NR = R == 64 ? 2 : 3;
     static constexpr uint32_t q = 0, p = 9 * R * 128, rope = p + R * 128, unit = rope + NR * kRope, bars = unit + NV * kUnit;
-    static constexpr uint32_t alpha = bars + (2 * NV + 2 * NR + 12) * 8, end = alpha + 64 * 4 + 64, bytes = end + 1024;
+    static constexpr uint32_t alpha = bars + (NV + NR + kFull + 12) * 8, end = alpha + 64 * 4 + 64, bytes = end + 1024;
     static constexpr uint32_t columns = R == 64 ? 512 : 256;            // of tensor memory: S twice 64, O 4 R
     static_assert(bytes <= 227 * 1024, "shared memory");
     static_assert(p % 1024 == 0 && rope % 1024 == 0 && unit % 1024 == 0, "swizzle atoms");
@@ -194,11 +196,10 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     const uint32_t sb = smem_u32(smem);
-    uint64_t* v_full = reinterpret_cast<uint64_t*>(smem + P::bars);      // [NV]
-    uint64_t* v_empty = v_full + P::NV;
-    uint64_t* r_full = v_empty + P::NV;                                  // [NR]
-    uint64_t* r_empty = r_full + P::NR;
-    uint64_t* q_full = r_empty + P::NR;
+    uint64_t* v_empty = reinterpret_cast<uint64_t*>(smem + P::bars);     // [NV]
+    uint64_t* r_empty = v_empty + P::NV;                                 // [NR]
+    uint64_t* t_full = r_empty + P::NR;                                  // [kFull]
+    uint64_t* q_full = t_full + kFull;
     uint64_t* q_empty = q_full + 1;
     uint64_t* s_full = q_empty + 1;                                      // [2]
     uint64_t* s_empty = s_full + 2;                                      // [2]
@@ -212,8 +213,9 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g = blockIdx.x / p.group, r = blockIdx.x % p.group;
     if (tid == 0) {
-        for (int i = 0; i < P::NV; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1); }
-        for (int i = 0; i < P::NR; ++i) { mbar_init(&r_full[i], 1); mbar_init(&r_empty[i], 1); }
+        for (int i = 0; i < P::NV; ++i) mbar_init(&v_empty[i], 1);
+        for (int i = 0; i < P::NR; ++i) mbar_init(&r_empty[i], 1);
+        for (int i = 0; i < kFull; ++i) mbar_init(&t_full[i], 1);
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
         for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&s_empty[i], 4); }
@@ -281,10 +283,12 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
     const uint32_t tmem = *s_tmem;
     const int NU = p.dl / 128;
 
-    if (warp == 0) {
-        // ============================================= loads: a warp walks, one lane of it issues
-        const int br = min(1 << p.s.page_shift, 64), boxes = 64 / br, outside = p.s.n_pages << p.s.page_shift;
-        RingAt v, ro;
+    if (warp == 0 || warp == 3) {
+        // ============================================= loads: warp 0 takes the first 64 columns of every unit, the rotated parts and Q, warp 3 the
+        // other 64.  A warp issues a copy every 100 clocks, and every 500 with an arrival between two of them (8 KB copies, one SM): so
+        // one barrier a tile, and two warps (a page of 16 makes 36 copies of a tile).
+        const int br = min(1 << p.s.page_shift, 64), boxes = 64 / br, outside = p.s.n_pages << p.s.page_shift, half = warp == 0 ? 0 : 1;
+        RingAt v, ro, f;
         uint32_t q_phase = 1;
         bool waited = false;
         while (w.next(p, g, r)) {
@@ -305,26 +309,28 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
 #pragma unroll
                 for (int b = 0; b < 4; ++b) y[b] = __shfl_sync(0xFFFFFFFFu, coord, (t * boxes - base + min(b, boxes - 1)) & 31);
                 role_wait(&r_empty[ro.slot], ro.phase ^ 1, p.status);
-                if (lane == 0) {
-                    mbar_expect_tx(&r_full[ro.slot], kRope);
-                    for (int b = 0; b < boxes; ++b) tma_2d(sb + P::rope + ro.slot * kRope + b * br * 128, &kv_map, p.dl, y[b], &r_full[ro.slot]);
+                if (half == 0 && elected()) {
+                    mbar_expect_tx(&t_full[f.slot], kRope + NU * kUnit);
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        if (b < boxes) tma_2d(sb + P::rope + ro.slot * kRope + b * br * 128, &kv_map, p.dl, y[b], &t_full[f.slot]);
                 }
                 ro.next(P::NR);
                 for (int u = 0; u < NU; ++u) {
                     role_wait(&v_empty[v.slot], v.phase ^ 1, p.status);
-                    if (lane == 0) {
-                        mbar_expect_tx(&v_full[v.slot], kUnit);
-                        for (int c = 0; c < 2; ++c)
-                            for (int b = 0; b < boxes; ++b)
-                                tma_2d(sb + P::unit + v.slot * kUnit + c * kRope + b * br * 128, &kv_map, u * 128 + c * 64, y[b], &v_full[v.slot]);
+                    if (elected()) {
+#pragma unroll
+                        for (int b = 0; b < 4; ++b)
+                            if (b < boxes) tma_2d(sb + P::unit + v.slot * kUnit + half * kRope + b * br * 128, &kv_map, u * 128 + half * 64, y[b], &t_full[f.slot]);
                     }
                     v.next(P::NV);
                 }
-                if (t == w.t0) {                                         // (behind the first tile: that does not wait for the kernel before)
+                f.next(kFull);
+                if (half == 0 && t == w.t0) {                            // (behind the first tile: that does not wait for the kernel before)
                     if (!waited) { pdl_wait_prior_grid(); waited = true; }
                     role_wait(q_empty, q_phase, p.status);
                     q_phase ^= 1;
-                    if (lane == 0) {
+                    if (elected()) {
                         mbar_expect_tx(q_full, (p.dl / 64 + 1) * R * 128);
                         for (int c = 0; c <= p.dl / 64; ++c) tma_2d(sb + P::q + c * R * 128, &q_map, c * 64, w.row0, q_full);
                     }
@@ -339,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
         const uint32_t id_s = idesc_bf16(64, 64);
         const uint32_t dq = desc_lo(sb + P::q), dk0 = desc_lo(sb + P::unit), dr0 = desc_lo(sb + P::rope);
         const int rks = p.dr / 16;
-        RingAt ks, kr;
+        RingAt ks, kr, f;
         int n = 0;                                                       // tiles issued
         uint32_t q_phase = 0;
         while (w.next(p, g, r)) {
@@ -348,12 +354,12 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
             for (int t = w.t0; t < w.t1; ++t, ++n) {
                 const int buf = n & 1;
                 role_wait(&s_empty[buf], ((uint32_t)(n >> 1) & 1) ^ 1, p.status);
-                role_wait(&r_full[kr.slot], kr.phase, p.status);
+                role_wait(&t_full[f.slot], f.phase, p.status);
+                f.next(kFull);
                 uint32_t at[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
                     if (u < NU) {
-                        role_wait(&v_full[ks.slot], ks.phase, p.status);
                         at[u] = dk0 + ((ks.slot * kUnit) >> 4);
                         ks.next(P::NV);
                     }
@@ -507,7 +513,6 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                 if (held < 64) {
                     RingAt c = vt;
                     for (int u = 0; u < NU; ++u) {
-                        role_wait(&v_full[c.slot], c.phase, p.status);
                         uint8_t* unit = smem + P::unit + c.slot * kUnit;
                         for (int i = held * 8 + (tid - 128); i < 512; i += 128) {
                             *reinterpret_cast<uint4*>(unit + i * 16) = make_uint4(0, 0, 0, 0);
