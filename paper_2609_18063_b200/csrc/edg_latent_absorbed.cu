@@ -22,6 +22,7 @@
 namespace edg {
 
 constexpr int kGroupMost = 8;               // CTAs side by side at most; sequences of more rows come in several units
+constexpr int kPiece = 2;                   // tiles that a piece costs beside its own: queries, epilogue, nothing overlapped
 constexpr int kSms = 148;                   // CTAs of the attention kernel: one to an SM
 
 inline int absorbed_rows(int64_t most_rows) { return most_rows <= 16 ? 16 : (most_rows <= 32 ? 32 : 64); }
@@ -56,7 +57,8 @@ __device__ __forceinline__ Seq sequence(const AbsorbedParams& p, int i) {
     q.kt = (q.len + 63) >> 6;
     return q;
 }
-// tiles that a group takes of a line of W
+// places on the line that a unit takes: its tiles, behind kPiece that stand for what a piece costs beside them; and a group's share of a line of W
+__device__ __forceinline__ long long unit_length(const Seq& q) { return q.kt > 0 ? q.kt + kPiece : 0; }
 __device__ __forceinline__ long long stretch(long long W, int groups) { return (W + groups - 1) / groups; }
 
 // ---------------------------------------------------------------- queries to the latent space
@@ -76,7 +78,7 @@ __global__ void __launch_bounds__(128) absorb_kernel(const __grid_constant__ Abs
         bool ok = tid != 0 || (p.s.cu[0] == 0 && p.s.cu[p.s.n] <= p.s.T);
         for (int i = i0; i < i1; ++i) {
             const Seq q = sequence(p, i);
-            t += (long long)q.units * q.kt;
+            t += q.units * unit_length(q);
             u += q.units;
             ok = ok && p.s.cu[i + 1] >= q.a && q.fresh <= p.max_new && q.len >= p.s.lens[i];
         }
@@ -91,7 +93,7 @@ __global__ void __launch_bounds__(128) absorb_kernel(const __grid_constant__ Abs
             const Seq q = sequence(p, i);
             p.tile_pre[i] = t;
             p.unit_pre[i] = u;
-            t += (long long)q.units * q.kt;
+            t += q.units * unit_length(q);
             u += q.units;
             if (i == p.s.n - 1) { p.tile_pre[p.s.n] = t; p.unit_pre[p.s.n] = u; }
         }
@@ -164,7 +166,7 @@ template <int R> struct Plan {
 
 // The pieces of a CTA, one after the other; every role walks them for itself.
 struct Walk {
-    int seq, unit, ug, tile;
+    int seq, unit, ug, tile;    // tile: place within the unit's part of the line
     long long left;
     Seq q;
     // the piece
@@ -173,16 +175,17 @@ struct Walk {
         while (left > 0 && seq < p.s.n) {
             q = sequence(p, seq);
             if (ug >= q.units || q.kt == 0) { unit += q.units - ug; ++seq; ug = 0; tile = 0; continue; }
-            t0 = tile;
-            t1 = (int)min((long long)q.kt, t0 + left);
-            left -= t1 - t0;
+            const int end = (int)min((long long)q.kt + kPiece, tile + left);
+            left -= end - tile;
+            t0 = max(tile - kPiece, 0);
+            t1 = max(end - kPiece, 0);
             slot = g + unit;
             const int first = (ug * p.group + r) * p.R;
             row0 = q.a * p.heads + first;
             rows = min(q.rows - first, p.R);
-            tile = t1;
-            if (tile == q.kt) { tile = 0; ++ug; ++unit; }
-            if (rows > 0) { first_row = first; return true; }
+            tile = end;
+            if (tile == q.kt + kPiece) { tile = 0; ++ug; ++unit; }
+            if (rows > 0 && t1 > t0) { first_row = first; return true; }
         }
         return false;
     }
@@ -233,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
         int u = 0;
         for (int i = i0; i < i1; ++i) {
             const Seq q = sequence(p, i);
-            t += (long long)q.units * q.kt;
+            t += q.units * unit_length(q);
             u += q.units;
         }
         long long xt = t;
@@ -259,13 +262,13 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
         if (end > start && t > 0 && before <= start && start < before + t) {
             for (int i = i0; i < i1; ++i) {
                 const Seq q = sequence(p, i);
-                const long long here = (long long)q.units * q.kt;
+                const long long here = q.units * unit_length(q);
                 if (start < before + here) {
-                    const int ug = (int)((start - before) / q.kt);
+                    const int ug = (int)((start - before) / unit_length(q));
                     s_at[0] = i;
                     s_at[1] = ug;
                     s_at[2] = ub + ug;
-                    s_from[0] = (start - before) % q.kt;
+                    s_from[0] = start - before - ug * unit_length(q);
                     break;
                 }
                 before += here;
@@ -295,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
             const int32_t* table = p.s.table + (size_t)w.seq * p.s.max_pages;
             int base = -64, coord = 0;                                   // boxes base .. base + 31 are known, one to a lane
             for (int t = w.t0; t < w.t1; ++t) {
-                if (t * boxes - base + boxes > 32) {
+                if ((t + 1) * boxes - base > 32) {
                     base = t * boxes;
                     const int at = (base + lane) * br;                   // first position of the lane's box
                     coord = outside;
@@ -561,121 +564,109 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
 
 // ---------------------------------------------------------------- sums of the pieces, and out of the latent space
 
-// A CTA: one head of 16 rows.  The latent sums go into shared memory as two bf16 parts, 16 bits of them in all.
-__global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ AbsorbedParams p) {
+constexpr int kCombine = 512;
+
+// A CTA: one head of 16 rows.  A warp adds up the pieces of a row and leaves its latent sums in shared memory as two bf16 parts, 16 bits of
+// them in all; then every warp takes eight values of W_uv, whose rows it has asked for before anything else.
+__global__ void __launch_bounds__(kCombine, 1) combine_kernel(const __grid_constant__ AbsorbedParams p) {
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ int s_first[16], s_count[16], s_row[16];      // first slot, pieces, row of a slot
     __shared__ float s_weight[16][kSms];
+    __shared__ int s_there[16];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
-    const int h = blockIdx.x, t0 = blockIdx.y * 16, pitch = p.dl * 2 + 64;
-    for (int i = tid; i < p.dv * p.dl / 64; i += 256)        // (this head's part of W_uv comes into L2 while the pieces are being made)
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(p.W_uv + (size_t)h * p.dv * p.dl + (size_t)i * 64));
+    const int h = blockIdx.x, t0 = blockIdx.y * 16, pitch = p.dl * 2 + 64, kb = p.dl / 32;
+    const bool values = warp * 8 < p.dv;
+    // lane t4 of a quad takes columns 8 t4 .. 8 t4 + 7 of every 32, of both operands: any order of k will do
+    uint4 w[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+        if (values && k < kb) w[k] = __ldg(reinterpret_cast<const uint4*>(p.W_uv + ((size_t)h * p.dv + warp * 8 + g) * p.dl + t4 * 8 + k * 32));
     pdl_wait_prior_grid();
-    if (tid < 16) {
-        const int t = t0 + tid;
-        int row = -1, first = 0, count = 0;
-        if (t < p.s.T) {
-            int lo = 0, hi = p.s.n;                                      // ends cu[1..n] that are <= t
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (p.s.cu[mid + 1] <= t) lo = mid + 1; else hi = mid;
-            }
-            if (lo < p.s.n) {
-                const Seq q = sequence(p, lo);
-                const int in = (t - q.a) * p.heads + h, rt = in / p.R, ug = rt / p.group;
-                if (t >= q.a) {
-                    row = (rt - ug * p.group) * p.R + in - rt * p.R;
-                    if (q.kt > 0) {
-                        const long long each = stretch(p.tile_pre[p.s.n], p.groups), a = p.tile_pre[lo] + (long long)ug * q.kt;
-                        const int g0 = (int)(a / each), g1 = (int)((a + q.kt - 1) / each);
-                        first = g0 + p.unit_pre[lo] + ug;
-                        count = max(min(g1 - g0 + 1, p.max_slots - first), 0);
-                    }
-                }
-            }
-        }
-        s_row[tid] = row;
-        s_first[tid] = first;
-        s_count[tid] = count;
-    }
-    __syncthreads();
     {
-        const int i = tid >> 4, k0 = tid & 15, c0 = k0 * 4, row = s_row[i], count = s_count[i];
-        const size_t step = (size_t)p.group * p.R, at = (size_t)s_first[i] * step + row;
+        const int t = t0 + warp;
+        int first = 0, count = 0, row = -1;
+        const int seq = t < p.s.T ? find_sequence(p.s.cu, p.s.n, t, lane) : p.s.n;
+        if (seq < p.s.n) {
+            const Seq q = sequence(p, seq);
+            const long long W = p.tile_pre[p.s.n], before = p.tile_pre[seq];
+            const int units = p.unit_pre[seq], in = (t - q.a) * p.heads + h, rt = in / p.R, ug = rt / p.group;
+            row = (rt - ug * p.group) * p.R + in - rt * p.R;
+            if (q.kt > 0) {
+                const long long each = stretch(W, p.groups), at = before + ug * unit_length(q) + kPiece;
+                const int g0 = (int)(at / each), g1 = (int)((at + q.kt - 1) / each);
+                first = g0 + units + ug;
+                count = max(min(g1 - g0 + 1, p.max_slots - first), 0);
+            }
+        }
+        const size_t step = (size_t)p.group * p.R, at = (size_t)first * step + row;
         // weights of the pieces: 2^(m - largest m)
-        float top = -INFINITY;
-        for (int k = k0; k < count; k += 16) {
-            const float v = p.ml[at + k * step].x;
-            s_weight[i][k] = v;
-            top = fmaxf(top, v);
-        }
+        float2 ml[(kSms + 31) / 32];
+        float top = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+        for (int k = 0; k < (kSms + 31) / 32; ++k)
+            if (k * 32 + lane < count) {
+                ml[k] = p.ml[at + (k * 32 + lane) * step];
+                top = fmaxf(top, ml[k].x);
+            }
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
         const float mm = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
-        for (int k = k0; k < count; k += 16) {
-            const float e = exp2f(s_weight[i][k] - mm);
-            s_weight[i][k] = e;
-            sum = fmaf(p.ml[at + k * step].y, e, sum);
-        }
-        sum = group_sum<16>(sum);
+#pragma unroll
+        for (int k = 0; k < (kSms + 31) / 32; ++k)
+            if (k * 32 + lane < count) {
+                const float e = exp2f(ml[k].x - mm);
+                s_weight[warp][k * 32 + lane] = e;
+                sum = fmaf(ml[k].y, e, sum);
+            }
+        sum = warp_sum(sum);
+        if (lane == 0) s_there[warp] = row >= 0;
         __syncwarp();
-        float4 o[8];
+        float4 o[4];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
+        for (int k = 0; k < 4; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
         for (int j = 0; j < count; ++j) {
-            const float e = s_weight[i][j];
-            const float4* src = reinterpret_cast<const float4*>(p.part + (at + j * step) * p.dl + c0);
+            const float e = s_weight[warp][j];
+            const float4* src = reinterpret_cast<const float4*>(p.part + (at + j * step) * p.dl) + lane;
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (k * 64 < p.dl) {
-                    const float4 v = __ldcs(src + k * 16);
+            for (int k = 0; k < 4; ++k)
+                if (k * 128 < p.dl) {
+                    const float4 v = __ldcs(src + k * 32);
                     o[k].x = fmaf(v.x, e, o[k].x); o[k].y = fmaf(v.y, e, o[k].y); o[k].z = fmaf(v.z, e, o[k].z); o[k].w = fmaf(v.w, e, o[k].w);
                 }
         }
         const float inv = sum == 0.f ? 0.f : 1.f / sum;                  // (nothing seen: zeros; NaN stays)
-        uint8_t* hi = smem + i * pitch + c0 * 2;
+        uint8_t* hi = smem + warp * pitch + lane * 8;
         uint8_t* lo = hi + 16 * pitch;
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k * 64 < p.dl) {
+        for (int k = 0; k < 4; ++k)
+            if (k * 128 < p.dl) {
                 const float x = o[k].x * inv, y = o[k].y * inv, z = o[k].z * inv, u = o[k].w * inv;
                 const uint32_t h0 = bf16_pair(x, y), h1 = bf16_pair(z, u);
-                *reinterpret_cast<uint2*>(hi + k * 128) = make_uint2(h0, h1);
-                *reinterpret_cast<uint2*>(lo + k * 128) = make_uint2(bf16_pair(x - bf16_lo(h0), y - bf16_hi(h0)), bf16_pair(z - bf16_lo(h1), u - bf16_hi(h1)));
+                *reinterpret_cast<uint2*>(hi + k * 256) = make_uint2(h0, h1);
+                *reinterpret_cast<uint2*>(lo + k * 256) = make_uint2(bf16_pair(x - bf16_lo(h0), y - bf16_hi(h0)), bf16_pair(z - bf16_lo(h1), u - bf16_hi(h1)));
             }
     }
     __syncthreads();
-    const int v0 = warp * 16;
-    if (v0 >= p.dv) return;
-    // lane t4 of a quad takes columns 8 t4 .. 8 t4 + 7 of every 32, of both operands: any order of k will do
-    float d[2][4] = {};
-    const uint16_t* w0 = p.W_uv + ((size_t)h * p.dv + v0 + g) * p.dl + t4 * 8;
+    if (!values) return;
+    float d[4][4] = {};                                                  // (four chains of products, by part and half of a block)
     const uint8_t* a0 = smem + g * pitch + t4 * 16;
-#pragma unroll 4
-    for (int k = 0; k < p.dl / 32; ++k) {
-        const uint4 b0 = __ldg(reinterpret_cast<const uint4*>(w0 + k * 32)), b1 = __ldg(reinterpret_cast<const uint4*>(w0 + 8 * (size_t)p.dl + k * 32));
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            const uint8_t* a = a0 + part * 16 * pitch + k * 64;
-            const uint4 x = *reinterpret_cast<const uint4*>(a), z = *reinterpret_cast<const uint4*>(a + 8 * pitch);
-            mma16816_bf16(d[0], x.x, z.x, x.y, z.y, b0.x, b0.y);
-            mma16816_bf16(d[0], x.z, z.z, x.w, z.w, b0.z, b0.w);
-            mma16816_bf16(d[1], x.x, z.x, x.y, z.y, b1.x, b1.y);
-            mma16816_bf16(d[1], x.z, z.z, x.w, z.w, b1.z, b1.w);
-        }
-    }
+    for (int k = 0; k < 16; ++k)
+        if (k < kb)
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                const uint8_t* a = a0 + part * 16 * pitch + k * 64;
+                const uint4 x = *reinterpret_cast<const uint4*>(a), z = *reinterpret_cast<const uint4*>(a + 8 * pitch);
+                mma16816_bf16(d[part * 2], x.x, z.x, x.y, z.y, w[k].x, w[k].y);
+                mma16816_bf16(d[part * 2 + 1], x.z, z.z, x.w, z.w, w[k].z, w[k].w);
+            }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        if (s_row[g + 8 * e] < 0) continue;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const size_t at = ((size_t)(t0 + g + 8 * e) * p.heads + h) * p.dv + v0 + j * 8 + 2 * t4;
-            const float x = d[j][2 * e], y = d[j][2 * e + 1];
-            if (p.out_dtype == EDG_F16) *reinterpret_cast<__half2*>(static_cast<__half*>(p.y) + at) = __floats2half2_rn(x, y);
-            else *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.y) + at) = bf16_pair(x, y);
-        }
+        if (s_there[g + 8 * e] == 0) continue;
+        const size_t at = ((size_t)(t0 + g + 8 * e) * p.heads + h) * p.dv + warp * 8 + 2 * t4;
+        const float x = (d[0][2 * e] + d[1][2 * e]) + (d[2][2 * e] + d[3][2 * e]), y = (d[0][2 * e + 1] + d[1][2 * e + 1]) + (d[2][2 * e + 1] + d[3][2 * e + 1]);
+        if (p.out_dtype == EDG_F16) *reinterpret_cast<__half2*>(static_cast<__half*>(p.y) + at) = __floats2half2_rn(x, y);
+        else *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.y) + at) = bf16_pair(x, y);
     }
 }
 
@@ -756,7 +747,7 @@ int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new,
     EDG_CUDA_TRY(L.R == 16   ? launch_pdl(absorbed_kernel<16>, grid, kThreads, Plan<16>::bytes, st, p, kv_map, q_map)
                  : L.R == 32 ? launch_pdl(absorbed_kernel<32>, grid, kThreads, Plan<32>::bytes, st, p, kv_map, q_map)
                              : launch_pdl(absorbed_kernel<64>, grid, kThreads, Plan<64>::bytes, st, p, kv_map, q_map));
-    EDG_CUDA_TRY(launch_pdl(combine_kernel, dim3(d.heads, (s.T + 15) / 16), 256, (size_t)32 * (d.d_latent * 2 + 64), st, p));
+    EDG_CUDA_TRY(launch_pdl(combine_kernel, dim3(d.heads, (s.T + 15) / 16), kCombine, (size_t)32 * (d.d_latent * 2 + 64), st, p));
     return EDG_OK;
 }
 
