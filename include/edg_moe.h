@@ -532,7 +532,7 @@ typedef struct edg_latent_desc {
 } edg_latent_desc;
 
 /* Bytes of device scratch for calls with up to n_seqs sequences, T new rows in all, max_new of one sequence, total_len positions in
- * all.  First 4096 bytes: control block as elsewhere (zeroed once by the caller, status word).  None of the arguments makes it fall. */
+ * all (T and n_seqs at most 65535, total_len below 2^31).  First 4096 bytes: control block as elsewhere (zeroed once by the caller, status word).  None of the arguments makes it fall. */
 int32_t edg_latent_workspace_bytes(const edg_latent_desc* desc, int32_t n_seqs, int32_t T, int32_t max_new, int64_t total_len, size_t* bytes);
 
 /* New rows of the cache.  Sequence i has the new rows cu[i] .. cu[i+1] - 1 (dev int32 [n_seqs + 1], cu[0] = 0, not falling; cu[n_seqs] <= T: rows

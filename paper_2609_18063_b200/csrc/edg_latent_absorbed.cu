@@ -41,7 +41,7 @@ struct AbsorbedParams {
     int64_t ldq, ldr;
     float scale;
     int R, group, groups, max_slots;
-    int max_new;
+    int max_new, most;          // the caller's bound; sequences of up to `most` new rows are taken
 };
 
 namespace {
@@ -52,7 +52,7 @@ __device__ __forceinline__ Seq sequence(const AbsorbedParams& p, int i) {
     q.a = p.s.cu[i];
     q.fresh = max(p.s.cu[i + 1] - q.a, 0);
     q.len = min(max(p.s.lens[i], 0), p.s.max_pages << p.s.page_shift);
-    q.rows = q.fresh * p.heads;
+    q.rows = q.fresh <= p.most ? q.fresh * p.heads : 0;
     q.units = ((q.rows + p.R - 1) / p.R + p.group - 1) / p.group;
     q.kt = (q.len + 63) >> 6;
     return q;
@@ -114,6 +114,10 @@ __global__ void __launch_bounds__(128) absorb_kernel(const __grid_constant__ Abs
             if (k * 16 < p.dn) *reinterpret_cast<uint4*>(s_w + (k * 16 + (tid >> 3)) * kPitch + (tid & 7) * 8) = v[k];
     }
     const int t_end = min(p.s.T, ((int)blockIdx.y + 1) * 64);
+    if (p.most < p.max_new) {                                           // rows of one sequence that the other form takes
+        const int a = find_sequence(p.s.cu, p.s.n, blockIdx.y * 64, lane), b = find_sequence(p.s.cu, p.s.n, t_end - 1, lane);
+        if (a == b && (a == p.s.n || sequence(p, a).rows == 0)) return;
+    }
     if (c0 == 0)                                                        // the rotated part, zeros behind it
         for (int i = tid; i < (t_end - (int)blockIdx.y * 64) * 8; i += 128) {
             const int t = blockIdx.y * 64 + (i >> 3), c = (i & 7) * 8;
@@ -585,8 +589,8 @@ __global__ void __launch_bounds__(kCombine, 1) combine_kernel(const __grid_const
         const int t = t0 + warp;
         int first = 0, count = 0, row = -1;
         const int seq = t < p.s.T ? find_sequence(p.s.cu, p.s.n, t, lane) : p.s.n;
-        if (seq < p.s.n) {
-            const Seq q = sequence(p, seq);
+        const Seq q = seq < p.s.n ? sequence(p, seq) : Seq{};
+        if (q.rows > 0) {
             const long long W = p.tile_pre[p.s.n], before = p.tile_pre[seq];
             const int units = p.unit_pre[seq], in = (t - q.a) * p.heads + h, rt = in / p.R, ug = rt / p.group;
             row = (rt - ug * p.group) * p.R + in - rt * p.R;
@@ -694,11 +698,11 @@ AbsorbedLayout absorbed_layout(const edg_latent_desc& d, int n_seqs, int T, int 
 
 }  // namespace
 
-size_t absorbed_workspace(const edg_latent_desc& d, int n_seqs, int T, int max_new) { return absorbed_layout(d, n_seqs, T, max_new).bytes; }
+size_t absorbed_workspace(const edg_latent_desc& d, int n_seqs, int T, int most) { return absorbed_layout(d, n_seqs, T, most).bytes; }
 
-int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new, const void* q, const void* q_rope, const void* W_uk, const void* W_uv,
+int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new, int most, const void* q, const void* q_rope, const void* W_uk, const void* W_uv,
                      const void* cache, void* y, void* workspace, cudaStream_t st) {
-    const AbsorbedLayout L = absorbed_layout(d, s.n, s.T, max_new);
+    const AbsorbedLayout L = absorbed_layout(d, s.n, s.T, most);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     AbsorbedParams p = {};
     p.s = s;
@@ -728,6 +732,7 @@ int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new,
     p.groups = L.groups;
     p.max_slots = L.slots;
     p.max_new = max_new;
+    p.most = most;
     static OncePerDevice once;
     EDG_CUDA_TRY(once([] {
         cudaError_t e = allow_smem(Plan<16>::bytes, absorbed_kernel<16>);

@@ -1,0 +1,591 @@
+// Latent attention, expanded form (prompts): keys and values of every head are written out once, then plain causal attention over them.
+//
+//     K[h,j] = W_uk[h] c_j,  V[h,j] = W_uv[h] c_j            (expand_kernel: one product of 128 cache rows with a head's weights each)
+//     y[t,h] = softmax(scale (q_nope . K[h,j] + q_rope . p_j)) V[h]        (prompt_kernel)
+//
+// 2 (d_n + d_r + d_v) operations a pair of rows against 2 (2 d_l + d_r) in the latent space, 3.4 times fewer at 128 / 64 / 128 / 512; the writing out costs
+// 2 d_l (d_n + d_v) a position and head, which some hundred new rows a sequence earn back.
+//
+// prompt_kernel: a CTA takes two tiles of 128 new rows of one head; while the softmax of one runs, the tensor cores work on the other.  S of
+// a tile (128 x 128) lies in tensor memory, a row to a lane: maximum and sum are a thread's own.  P goes back over S as bf16 and is the A
+// operand of P V from there.  O is rescaled only when a row's maximum has grown by more than 2^8.  Keys and values come by
+// TMA in chunks of 64 columns through one ring of eight (K of a tile, V of it, K of the next: the tile after that takes what S has read).
+// Positions behind a sequence's end are padded to 128; their values are written as zeros, their scores never looked at.
+#include "edg_latent.cuh"
+#include "edg_umma.cuh"
+
+namespace edg {
+
+struct ExpandedParams {
+    LatentSeqs s;
+    const uint16_t* cache;
+    uint16_t *K, *V, *Rp;       // [heads][rows][dn], [heads][rows][dv], [rows][64] (rotated part and zeros)
+    int32_t *q_pre, *kv_pre;    // [n + 1] pairs of row tiles before a sequence; tiles of 128 positions before it
+    void* y;
+    int32_t* status;
+    int heads, dn, dr, dv, dl, out_dtype;
+    int rows;                   // rows of K and V that there is room for, a multiple of 128
+    int more_than;              // sequences of more new rows than this are taken
+    int max_new, splits;
+    int64_t total_len;
+    float scale;
+};
+
+namespace {
+
+struct XSeq { int a, fresh, len, pairs, tiles; };
+__device__ __forceinline__ XSeq xsequence(const ExpandedParams& p, int i) {
+    XSeq q;
+    q.a = p.s.cu[i];
+    q.fresh = max(min(p.s.cu[i + 1], p.s.T) - q.a, 0);
+    q.len = min(max(p.s.lens[i], 0), p.s.max_pages << p.s.page_shift);
+    const bool mine = q.fresh > p.more_than;
+    q.pairs = mine ? (q.fresh + 255) >> 8 : 0;
+    q.tiles = mine ? (q.len + 127) >> 7 : 0;
+    return q;
+}
+
+// prefix sums over the sequences, and the caller's bounds
+__global__ void __launch_bounds__(256) prompt_plan_kernel(const __grid_constant__ ExpandedParams p) {
+    pdl_launch_dependents();
+    __shared__ int s_q[256], s_k[256];
+    __shared__ long long s_l[256];
+    const int tid = threadIdx.x, per = (p.s.n + 255) / 256, i0 = min(tid * per, p.s.n), i1 = min(i0 + per, p.s.n);
+    int q = 0, k = 0;
+    long long len = 0;
+    bool ok = tid != 0 || (p.s.cu[0] == 0 && p.s.cu[p.s.n] <= p.s.T);
+    for (int i = i0; i < i1; ++i) {
+        const XSeq x = xsequence(p, i);
+        q += x.pairs;
+        k += x.tiles;
+        len += x.len;
+        ok = ok && p.s.cu[i + 1] >= x.a && p.s.cu[i + 1] - x.a <= p.max_new && x.len >= p.s.lens[i];
+    }
+    s_q[tid] = q;
+    s_k[tid] = k;
+    s_l[tid] = len;
+    __syncthreads();
+    q = k = 0;
+    len = 0;
+    for (int j = 0; j < 256; ++j) {
+        if (j < tid) { q += s_q[j]; k += s_k[j]; }
+        len += s_l[j];
+    }
+    if (!ok || len > p.total_len) latent_raise(p.status, EDG_E_RANGE);
+    for (int i = i0; i < i1; ++i) {
+        const XSeq x = xsequence(p, i);
+        p.q_pre[i] = q;
+        p.kv_pre[i] = k;
+        q += x.pairs;
+        k += x.tiles;
+        if (i == p.s.n - 1) { p.q_pre[p.s.n] = q; p.kv_pre[p.s.n] = k; }
+    }
+    if (k * 128ll > p.rows && tid == 255) latent_raise(p.status, EDG_E_RANGE);
+}
+
+// ---------------------------------------------------------------- keys and values
+
+constexpr int kXThreads = 256;              // warp 0 loads, warp 1 issues products, warps 4-7 write out
+constexpr int kXRing = 5;
+constexpr uint32_t kChunk = 16384;          // 128 rows of 64 columns
+constexpr uint32_t kXW = 8 * kChunk, kXBars = kXW + kXRing * kChunk, kXBytes = kXBars + 256 + 1024;
+
+__global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_constant__ ExpandedParams p, const __grid_constant__ CUtensorMap c_map,
+                                                              const __grid_constant__ CUtensorMap uk_map, const __grid_constant__ CUtensorMap uv_map) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    const uint32_t sb = smem_u32(smem);
+    uint64_t* w_full = reinterpret_cast<uint64_t*>(smem + kXBars);       // [kXRing]
+    uint64_t* w_empty = w_full + kXRing;
+    uint64_t* c_full = w_empty + kXRing;
+    uint64_t* d_full = c_full + 1;                                       // [2]
+    uint64_t* d_empty = d_full + 2;                                      // [2]
+    uint32_t* s_tmem = reinterpret_cast<uint32_t*>(d_empty + 2);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int i = 0; i < kXRing; ++i) { mbar_init(&w_full[i], 1); mbar_init(&w_empty[i], 1); }
+        mbar_init(c_full, 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(&d_full[i], 1); mbar_init(&d_empty[i], 4); }
+        fence_barrier_init();
+    }
+    if (warp == 1) tmem_alloc(s_tmem, 256);
+    pdl_launch_dependents();
+    pdl_wait_prior_grid();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *s_tmem;
+    const int tile = blockIdx.x, split = blockIdx.y;
+    const int h0 = (int)((int64_t)p.heads * split / p.splits), h1 = (int)((int64_t)p.heads * (split + 1) / p.splits);
+    const bool there = tile < p.kv_pre[p.s.n] && (tile + 1) * 128 <= p.rows;
+    const int nc = p.dl / 64;
+    if (there) {
+        const int seq = find_sequence(p.kv_pre, p.s.n, tile, lane);
+        const XSeq q = xsequence(p, seq);
+        const int pos0 = (tile - p.kv_pre[seq]) * 128;
+        if (warp == 0) {
+            const int br = min(1 << p.s.page_shift, 128), boxes = 128 / br, outside = p.s.n_pages << p.s.page_shift;
+            int coord = outside;
+            const int at = pos0 + lane * br;
+            if (lane < boxes && at < q.len) {
+                const int pg = p.s.table[(size_t)seq * p.s.max_pages + (at >> p.s.page_shift)];
+                if (pg >= 0 && pg < p.s.n_pages) coord = (pg << p.s.page_shift) + (at & ((1 << p.s.page_shift) - 1));
+                else latent_raise(p.status, EDG_E_RANGE);
+            }
+            if (elected()) mbar_expect_tx(c_full, nc * kChunk);
+            __syncwarp();
+            for (int b = 0; b < boxes; ++b) {
+                const int y = __shfl_sync(0xFFFFFFFFu, coord, b);
+                if (elected())
+                    for (int c = 0; c < nc; ++c) tma_2d(sb + c * kChunk + b * br * 128, &c_map, c * 64, y, c_full);
+                __syncwarp();
+            }
+            RingAt w;
+            for (int h = h0; h < h1; ++h)
+                for (int kv = 0; kv < 2; ++kv)
+                    for (int c = 0; c < nc; ++c) {
+                        role_wait(&w_empty[w.slot], w.phase ^ 1, p.status);
+                        if (elected()) {
+                            const int n = kv == 0 ? p.dn : p.dv;
+                            tma_2d(sb + kXW + w.slot * kChunk, kv == 0 ? &uk_map : &uv_map, c * 64, h * n, &w_full[w.slot]);
+                            mbar_expect_tx(&w_full[w.slot], n * 128);
+                        }
+                        __syncwarp();
+                        w.next(kXRing);
+                    }
+        } else if (warp == 1) {
+            const uint32_t dc = desc_lo(sb), dw = desc_lo(sb + kXW);
+            RingAt w;
+            int j = 0;
+            role_wait(c_full, 0, p.status);
+            for (int h = h0; h < h1; ++h)
+                for (int kv = 0; kv < 2; ++kv, ++j) {
+                    const uint32_t id = idesc_bf16(128, kv == 0 ? p.dn : p.dv), d = tmem + (j & 1) * 128;
+                    role_wait(&d_empty[j & 1], ((uint32_t)(j >> 1) & 1) ^ 1, p.status);
+                    for (int c = 0; c < nc; ++c) {
+                        role_wait(&w_full[w.slot], w.phase, p.status);
+                        tc_fence_after();
+                        if (elected()) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                umma_ss(d, dc + ((c * kChunk + k * 32) >> 4), dw + ((w.slot * kChunk + k * 32) >> 4), id, c + k > 0);
+                            umma_done(&w_empty[w.slot]);
+                            if (c == nc - 1) umma_done(&d_full[j & 1]);
+                        }
+                        __syncwarp();
+                        w.next(kXRing);
+                    }
+                }
+        } else if (warp >= 4) {
+            const int wq = warp & 3, row = wq * 32 + lane;
+            const uint32_t lanes = (uint32_t)(wq * 32) << 16;
+            const bool held = pos0 + row < q.len;
+            if (split == 0) {                                            // the rotated part of this thread's row
+                uint4* out = reinterpret_cast<uint4*>(p.Rp + ((size_t)tile * 128 + row) * 64);
+                const int at = pos0 + row;
+                int pg = -1;
+                if (held) pg = p.s.table[(size_t)seq * p.s.max_pages + (at >> p.s.page_shift)];
+                const bool ok = pg >= 0 && pg < p.s.n_pages;
+                const uint4* src = reinterpret_cast<const uint4*>(
+                    p.cache + (((size_t)(ok ? pg : 0) << p.s.page_shift) + (at & ((1 << p.s.page_shift) - 1))) * (p.dl + p.dr) + p.dl);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) out[c] = ok && c * 8 < p.dr ? src[c] : make_uint4(0, 0, 0, 0);
+            }
+            int j = 0;
+            for (int h = h0; h < h1; ++h)
+                for (int kv = 0; kv < 2; ++kv, ++j) {
+                    const int n = kv == 0 ? p.dn : p.dv;
+                    uint16_t* out = (kv == 0 ? p.K : p.V) + ((size_t)h * p.rows + (size_t)tile * 128 + row) * n;
+                    role_wait(&d_full[j & 1], (uint32_t)(j >> 1) & 1, p.status);
+                    tc_fence_after();
+#pragma unroll 2
+                    for (int c = 0; c < n; c += 16) {
+                        uint32_t v[16];
+                        tmem_ld(tmem + lanes + (j & 1) * 128 + c, v);
+                        uint32_t o[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) o[i] = held ? bf16_pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])) : 0u;
+                        *reinterpret_cast<uint4*>(out + c) = make_uint4(o[0], o[1], o[2], o[3]);
+                        *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&d_empty[j & 1]);
+                }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) tmem_free(tmem, 256);
+}
+
+// ---------------------------------------------------------------- attention
+
+constexpr int kPThreads = 384;              // warp 0 loads, warp 1 issues products, warps 4-7 and 8-11 a tile of rows each
+constexpr int kPRing = 8;
+constexpr uint32_t kPQ = 0, kPRingAt = 6 * kChunk, kPBars = kPRingAt + kPRing * kChunk, kPBytes = kPBars + 512 + 1024;
+
+__global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_constant__ ExpandedParams p, const __grid_constant__ CUtensorMap qn_map,
+                                                              const __grid_constant__ CUtensorMap qr_map, const __grid_constant__ CUtensorMap k_map,
+                                                              const __grid_constant__ CUtensorMap r_map, const __grid_constant__ CUtensorMap v_map) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    const uint32_t sb = smem_u32(smem);
+    uint64_t* empty = reinterpret_cast<uint64_t*>(smem + kPBars);        // [kPRing] chunks that may be overwritten
+    uint64_t* kv_full = empty + kPRing;                                  // [kPRing] keys of a tile, its values, the next keys ...: never more than chunks
+    uint64_t* q_full = kv_full + kPRing;                                      // [2]
+    uint64_t* s_full = q_full + 2;                                       // [2]
+    uint64_t* p_full = s_full + 2;                                       // [2]
+    uint64_t* o_done = p_full + 2;                                       // [2]
+    uint32_t* s_tmem = reinterpret_cast<uint32_t*>(o_done + 2);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int i = 0; i < kPRing; ++i) mbar_init(&empty[i], 1);
+        for (int i = 0; i < kPRing; ++i) mbar_init(&kv_full[i], 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(&q_full[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); mbar_init(&o_done[i], 1); }
+        fence_barrier_init();
+    }
+    if (warp == 1) tmem_alloc(s_tmem, 512);
+    pdl_wait_prior_grid();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *s_tmem;
+    const int h = blockIdx.x % p.heads, pairs = p.q_pre[p.s.n];
+    const int pair = pairs - 1 - (int)(blockIdx.x / p.heads);                        // (the last rows of a sequence see the most: they go first)
+    const int seq = pair >= 0 ? find_sequence(p.q_pre, p.s.n, pair, lane) : p.s.n;
+    if (seq < p.s.n) {
+        const XSeq q = xsequence(p, seq);
+        const int r0 = (pair - p.q_pre[seq]) * 256, kv0 = p.kv_pre[seq] * 128;
+        const bool fits = kv0 + q.tiles * 128 <= p.rows;
+        const int pos0 = q.len - q.fresh + r0;                           // position of the pair's first row
+        int n[2];                                                        // tiles of 128 positions that a tile of rows sees something of
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int last = min(r0 + i * 128 + 127, q.fresh - 1);      // its last row
+            n[i] = fits && r0 + i * 128 < q.fresh ? max((q.len - q.fresh + last + 128) >> 7, 0) : 0;
+        }
+        const int nt = max(n[0], n[1]);
+        const int nkc = (p.dn + 63) / 64, nvc = (p.dv + 63) / 64;        // chunks of keys (and one of rotated parts), of values
+        if (warp == 0) {
+            // ========================================= loads
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (n[i] > 0 && elected()) {
+                    mbar_expect_tx(&q_full[i], (nkc + 1) * kChunk);
+                    for (int c = 0; c < nkc; ++c) tma_3d(sb + kPQ + (i * 3 + c) * kChunk, &qn_map, c * 64, h, q.a + r0 + i * 128, &q_full[i]);
+                    tma_3d(sb + kPQ + (i * 3 + nkc) * kChunk, &qr_map, 0, h, q.a + r0 + i * 128, &q_full[i]);
+                }
+            __syncwarp();
+            RingAt w, f;
+            for (int t = 0; t < nt; ++t) {
+                const int row = kv0 + t * 128;
+                for (int c = 0; c <= nkc; ++c) {
+                    role_wait(&empty[w.slot], w.phase ^ 1, p.status);
+                    if (elected()) {
+                        if (c == 0) mbar_expect_tx(&kv_full[f.slot], (nkc + 1) * kChunk);
+                        if (c < nkc) tma_3d(sb + kPRingAt + w.slot * kChunk, &k_map, c * 64, row, h, &kv_full[f.slot]);
+                        else tma_2d(sb + kPRingAt + w.slot * kChunk, &r_map, 0, row, &kv_full[f.slot]);
+                    }
+                    __syncwarp();
+                    w.next(kPRing);
+                }
+                f.next(kPRing);
+                for (int c = 0; c < nvc; ++c) {
+                    role_wait(&empty[w.slot], w.phase ^ 1, p.status);
+                    if (elected()) {
+                        if (c == 0) mbar_expect_tx(&kv_full[f.slot], nvc * kChunk);
+                        tma_3d(sb + kPRingAt + w.slot * kChunk, &v_map, c * 64, row, h, &kv_full[f.slot]);
+                    }
+                    __syncwarp();
+                    w.next(kPRing);
+                }
+                f.next(kPRing);
+            }
+        } else if (warp == 1) {
+            // ========================================= products.  For each tile of rows O += P V of a tile of positions, then S of the next
+            const uint32_t id_s = idesc_bf16(128, 128), id_o = idesc_bf16(128, p.dv, false, true);
+            const uint32_t dq = desc_lo(sb + kPQ), dk = desc_lo(sb + kPRingAt), dv = desc_lo(sb + kPRingAt, kChunk);
+            const int rks = p.dr / 16;
+            RingAt f;                                                    // the next group (keys or values) to wait for
+            int at = 0;                                                  // ring place of the next group
+            auto take = [&](int chunks) { const int a = at; at = (at + chunks) & (kPRing - 1); role_wait(&kv_full[f.slot], f.phase, p.status); f.next(kPRing); return a; };
+            auto scores = [&](int i, int k) {
+                if (elected()) {
+                    for (int c = 0; c < nkc; ++c) {
+                        const uint32_t a = dq + (((i * 3 + c) * kChunk) >> 4), b = dk + ((((k + c) & (kPRing - 1)) * kChunk) >> 4);
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) umma_ss(tmem + i * 128, a + s * 2, b + s * 2, id_s, c + s > 0);
+                    }
+                    const uint32_t a = dq + (((i * 3 + nkc) * kChunk) >> 4), b = dk + ((((k + nkc) & (kPRing - 1)) * kChunk) >> 4);
+#pragma unroll
+                    for (int s = 0; s < 4; ++s)
+                        if (s < rks) umma_ss(tmem + i * 128, a + s * 2, b + s * 2, id_s, true);
+                    umma_done(&s_full[i]);
+                }
+                __syncwarp();
+            };
+            auto release = [&](int k, int chunks) {
+                if (elected())
+                    for (int c = 0; c < chunks; ++c) umma_done(&empty[(k + c) & (kPRing - 1)]);
+                __syncwarp();
+            };
+            int k = 0;
+            if (nt > 0) {
+                k = take(nkc + 1);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (n[i] > 0) {
+                        role_wait(&q_full[i], 0, p.status);
+                        tc_fence_after();
+                        scores(i, k);
+                    }
+                release(k, nkc + 1);
+            }
+            for (int t = 0; t < nt; ++t) {
+                const int v = take(nvc);
+                if (t + 1 < nt) k = take(nkc + 1);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (t < n[i]) {
+                        role_wait(&p_full[i], (uint32_t)t & 1, p.status);
+                        tc_fence_after();
+                        if (elected()) {
+                            const bool whole = nvc == 1 || v + 1 < kPRing;     // (values that go round the ring's end: a chunk at a time)
+                            const uint32_t b = dv + ((v * kChunk) >> 4);
+                            const uint32_t o = tmem + 256 + i * 128, pt = tmem + i * 128;
+                            if (whole) {
+#pragma unroll
+                                for (int s = 0; s < 8; ++s) umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id_o, t > 0 || s > 0);
+                            } else {
+                                const uint32_t id0 = idesc_bf16(128, 64, false, true), id1 = idesc_bf16(128, p.dv - 64, false, true);
+#pragma unroll
+                                for (int s = 0; s < 8; ++s) {
+                                    umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id0, t > 0 || s > 0);
+                                    umma_ts(o + 64, pt + s * 8, dv + ((s * 2048) >> 4), id1, t > 0 || s > 0);
+                                }
+                            }
+                            umma_done(&o_done[i]);
+                        }
+                        __syncwarp();
+                    }
+                    if (t + 1 < n[i]) scores(i, k);
+                }
+                release(v, nvc);
+                if (t + 1 < nt) release(k, nkc + 1);
+            }
+        } else if (warp >= 4) {
+            // ========================================= softmax: a thread is a row
+            const int i = (warp >> 2) - 1, wq = warp & 3, row = i * 128 + wq * 32 + lane;
+            const uint32_t st = tmem + ((uint32_t)(wq * 32) << 16) + i * 128, ot = st + 256;
+            const float k2 = p.scale * 1.4426950408889634f;
+            const int pos = pos0 + row;                                  // positions 0 .. pos are seen
+            float m = -INFINITY, l = 0.f;
+            const int mine = i == 0 ? n[0] : n[1];
+            for (int t = 0; t < mine; ++t) {
+                role_wait(&s_full[i], (uint32_t)t & 1, p.status);
+                tc_fence_after();
+                const int seen = pos + 1 - t * 128;                      // of this tile
+                const bool part = __any_sync(0xFFFFFFFFu, seen < 128);
+                float mt = m;
+#pragma unroll
+                for (int c = 0; c < 128; c += 32) {
+                    uint32_t v[32];
+                    tmem_ld(st + c, v);
+                    if (part) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (c + j >= seen) v[j] = 0xFF800000u;
+                    }
+                    float a = -INFINITY, b = -INFINITY, d = -INFINITY, e = -INFINITY;
+                    if (k2 >= 0.f) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) {
+                            a = fmaxf(a, __uint_as_float(v[j])); b = fmaxf(b, __uint_as_float(v[j + 1]));
+                            d = fmaxf(d, __uint_as_float(v[j + 2])); e = fmaxf(e, __uint_as_float(v[j + 3]));
+                        }
+                        a = fmaxf(fmaxf(a, b), fmaxf(d, e));
+                        if (a != -INFINITY) mt = fmaxf(mt, a * k2);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (!part || c + j < seen) mt = fmaxf(mt, __uint_as_float(v[j]) * k2);
+                    }
+                }
+                if (t == 0) m = mt;
+                const bool grown = mt > m + 8.f;
+                if (__any_sync(0xFFFFFFFFu, grown)) {
+                    const float alpha = grown ? exp2_approx(m - mt) : 1.f;
+                    if (grown) { m = mt; l *= alpha; }
+                    role_wait(&o_done[i], (uint32_t)(t - 1) & 1, p.status);
+                    tc_fence_after();
+                    for (int c = 0; c < p.dv; c += 16) {
+                        uint32_t v[16];
+                        tmem_ld(ot + c, v);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * alpha);
+                        tmem_st(ot + c, v);
+                    }
+                }
+                const float mm = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                for (int c = 0; c < 128; c += 32) {
+                    uint32_t v[32], o[16];
+                    tmem_ld(st + c, v);
+                    float la = 0.f, lb = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        float a = exp2_approx(fmaf(__uint_as_float(v[j]), k2, -mm)), b = exp2_approx(fmaf(__uint_as_float(v[j + 1]), k2, -mm));
+                        if (part) {
+                            if (c + j >= seen) a = 0.f;
+                            if (c + j + 1 >= seen) b = 0.f;
+                        }
+                        o[j / 2] = bf16_pair(a, b);
+                        la += a;
+                        lb += b;
+                    }
+                    l += la + lb;
+                    tmem_st(st + c / 2, o);                              // (over columns that have been read)
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[i]);
+            }
+            // ---- out
+            const bool have = r0 + row < q.fresh && fits;
+            if (mine > 0) {
+                role_wait(&o_done[i], (uint32_t)(mine - 1) & 1, p.status);
+                tc_fence_after();
+            }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const size_t out = ((size_t)(q.a + r0 + row) * p.heads + h) * p.dv;
+            for (int c = 0; c < p.dv; c += 16) {
+                uint32_t v[16], o[8];
+                if (mine > 0) tmem_ld(ot + c, v);
+                else
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[j] = 0u;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float a = l == 0.f ? 0.f : __uint_as_float(v[2 * j]) * inv, b = l == 0.f ? 0.f : __uint_as_float(v[2 * j + 1]) * inv;
+                    if (p.out_dtype == EDG_F16) {
+                        const __half2 x = __floats2half2_rn(a, b);
+                        o[j] = *reinterpret_cast<const uint32_t*>(&x);
+                    } else o[j] = bf16_pair(a, b);
+                }
+                if (have) {
+                    uint4* y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y) + out + c);
+                    y[0] = make_uint4(o[0], o[1], o[2], o[3]);
+                    y[1] = make_uint4(o[4], o[5], o[6], o[7]);
+                }
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) tmem_free(tmem, 512);
+}
+
+struct ExpandedLayout { int rows; size_t q_pre, kv_pre, K, V, Rp, bytes; };
+
+ExpandedLayout expanded_layout(const edg_latent_desc& d, int n_seqs, int T, int64_t total_len) {
+    ExpandedLayout L;
+    const int64_t with = n_seqs < T ? n_seqs : T, rows = (total_len + 127) / 128 * 128 + 128 * with;
+    L.rows = (int)(rows < 0x7FFFFF00 ? rows : 0x7FFFFF00);
+    L.q_pre = 0;
+    L.kv_pre = round_up(((size_t)n_seqs + 1) * 4, 256);
+    L.Rp = 2 * L.kv_pre;
+    L.K = L.Rp + (size_t)rows * 128;
+    L.V = round_up(L.K + (size_t)rows * d.heads * d.d_nope * 2, 256);
+    L.bytes = round_up(L.V + (size_t)rows * d.heads * d.d_v * 2, 256);
+    return L;
+}
+
+}  // namespace
+
+size_t expanded_workspace(const edg_latent_desc& d, int n_seqs, int T, int64_t total_len) { return expanded_layout(d, n_seqs, T, total_len).bytes; }
+
+int32_t run_expanded(const edg_latent_desc& d, const LatentSeqs& s, int max_new, int64_t total_len, int more_than, const void* q, const void* q_rope,
+                     const void* W_uk, const void* W_uv, const void* cache, void* y, int32_t* status, void* scratch, cudaStream_t st) {
+    const ExpandedLayout L = expanded_layout(d, s.n, s.T, total_len);
+    uint8_t* ws = static_cast<uint8_t*>(scratch);
+    ExpandedParams p = {};
+    p.s = s;
+    p.cache = static_cast<const uint16_t*>(cache);
+    p.K = reinterpret_cast<uint16_t*>(ws + L.K);
+    p.V = reinterpret_cast<uint16_t*>(ws + L.V);
+    p.Rp = reinterpret_cast<uint16_t*>(ws + L.Rp);
+    p.q_pre = reinterpret_cast<int32_t*>(ws + L.q_pre);
+    p.kv_pre = reinterpret_cast<int32_t*>(ws + L.kv_pre);
+    p.y = y;
+    p.status = status;
+    p.heads = d.heads;
+    p.dn = d.d_nope;
+    p.dr = d.d_rope;
+    p.dv = d.d_v;
+    p.dl = d.d_latent;
+    p.out_dtype = d.out_dtype;
+    p.rows = L.rows;
+    p.more_than = more_than;
+    p.max_new = max_new;
+    p.total_len = total_len;
+    p.scale = d.scale;
+    // heads of a tile of positions are shared out until there is a CTA for every SM
+    const int tiles = L.rows / 128;
+    p.splits = 148 / tiles < 1 ? 1 : (148 / tiles > d.heads ? d.heads : 148 / tiles);
+    static OncePerDevice once;
+    EDG_CUDA_TRY(once([] {
+        const cudaError_t e = allow_smem(kXBytes, expand_kernel);
+        return e == cudaSuccess ? allow_smem(kPBytes, prompt_kernel) : e;
+    }));
+    CUtensorMap c_map, uk_map, uv_map, qn_map, qr_map, k_map, r_map, v_map;
+    const uint64_t row = (uint64_t)latent_row(d), dl = (uint64_t)d.d_latent, H = (uint64_t)d.heads, dn = (uint64_t)d.d_nope, dr = (uint64_t)d.d_rope,
+                   dv = (uint64_t)d.d_v, rows = (uint64_t)L.rows, T = (uint64_t)s.T, ldq = (uint64_t)latent_ldq(d);
+    {
+        const uint64_t dims[2] = {row, (uint64_t)d.n_pages * d.page};
+        const uint32_t box[2] = {64, (uint32_t)(d.page < 128 ? d.page : 128)};
+        EDG_CUDA_TRY(make_map(&c_map, cache, 2, dims, &row, box));
+    }
+    {
+        const uint64_t dims[2] = {dl, H * dn};
+        const uint32_t box[2] = {64, (uint32_t)dn};
+        EDG_CUDA_TRY(make_map(&uk_map, W_uk, 2, dims, &dl, box));
+    }
+    {
+        const uint64_t dims[2] = {dl, H * dv};
+        const uint32_t box[2] = {64, (uint32_t)dv};
+        EDG_CUDA_TRY(make_map(&uv_map, W_uv, 2, dims, &dl, box));
+    }
+    const uint32_t rows128[3] = {64, 128, 1}, tokens128[3] = {64, 1, 128};
+    {
+        const uint64_t dims[3] = {dn, H, T}, strides[2] = {dn + dr, ldq};
+        EDG_CUDA_TRY(make_map(&qn_map, q, 3, dims, strides, tokens128));
+    }
+    {
+        const uint64_t dims[3] = {dr, H, T}, own[2] = {dr, H * dr}, in_q[2] = {dn + dr, ldq};
+        EDG_CUDA_TRY(make_map(&qr_map, q_rope != nullptr ? q_rope : static_cast<const uint16_t*>(q) + dn, 3, dims, q_rope != nullptr ? own : in_q, tokens128));
+    }
+    {
+        const uint64_t dims[3] = {dn, rows, H}, strides[2] = {dn, rows * dn};
+        EDG_CUDA_TRY(make_map(&k_map, p.K, 3, dims, strides, rows128));
+    }
+    {
+        const uint64_t dims[3] = {dv, rows, H}, strides[2] = {dv, rows * dv};
+        EDG_CUDA_TRY(make_map(&v_map, p.V, 3, dims, strides, rows128));
+    }
+    {
+        const uint64_t dims[2] = {64, rows}, stride = 64;
+        EDG_CUDA_TRY(make_map(&r_map, p.Rp, 2, dims, &stride, rows128));
+    }
+    prompt_plan_kernel<<<1, 256, 0, st>>>(p);
+    EDG_CUDA_TRY(cudaGetLastError());
+    EDG_CUDA_TRY(launch_pdl(expand_kernel, dim3(tiles, p.splits), kXThreads, kXBytes, st, p, c_map, uk_map, uv_map));
+    const int with = s.n < s.T ? s.n : s.T;
+    EDG_CUDA_TRY(launch_pdl(prompt_kernel, dim3(d.heads * (s.T / 256 + with)), kPThreads, kPBytes, st, p, qn_map, qr_map, k_map, r_map, v_map));
+    return EDG_OK;
+}
+
+}  // namespace edg
