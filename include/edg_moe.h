@@ -528,7 +528,7 @@ typedef struct edg_latent_desc {
     int32_t form;         /* EDG_LATENT_AUTO, _ABSORBED or _EXPANDED (attention)                         */
     int32_t ldkv;         /* elements between rows of kv, a multiple of 8; 0 = d_latent + d_rope         */
     int32_t ldq;          /* elements between rows of q, a multiple of 8; 0 = heads * (d_nope + d_rope)  */
-    float   scale;        /* of the scores, usually 1 / sqrt(d_nope + d_rope)                            */
+    float   scale;        /* of the scores, positive; usually 1 / sqrt(d_nope + d_rope)                  */
 } edg_latent_desc;
 
 /* Bytes of device scratch for calls with up to n_seqs sequences, T new rows in all, max_new of one sequence, total_len positions in

@@ -15,6 +15,7 @@ inline int32_t check_latent(const edg_latent_desc* d) {
     if (d->out_dtype != EDG_F16 && d->out_dtype != EDG_BF16) return EDG_E_INVAL;
     if (d->rope_halves != 0 && d->rope_halves != 1) return EDG_E_INVAL;
     if (d->form < EDG_LATENT_AUTO || d->form > EDG_LATENT_EXPANDED) return EDG_E_INVAL;
+    if (!(d->scale > 0.f) || d->scale > 3.4e38f) return EDG_E_INVAL;
     if (d->ldkv != 0 && (d->ldkv < d->d_latent + d->d_rope || d->ldkv % 8 != 0)) return EDG_E_SHAPE;
     if (d->ldq != 0 && (d->ldq < d->heads * (d->d_nope + d->d_rope) || d->ldq % 8 != 0)) return EDG_E_SHAPE;
     return EDG_OK;

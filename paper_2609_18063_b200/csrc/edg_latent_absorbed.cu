@@ -35,6 +35,7 @@ struct AbsorbedParams {
     float2* ml;                 // [slots][group][R]: maximum (in powers of two), sum
     long long* tile_pre;        // [n + 1] tiles before a sequence
     int32_t* unit_pre;          // [n + 1] units before it
+    int32_t* row_pre;           // [n + 1] new rows before it, of the sequences that are taken
     void* y;
     int32_t* status;
     int heads, dn, dr, dv, dl, out_dtype, hr;
@@ -49,8 +50,8 @@ namespace {
 struct Seq { int a, rows, len, fresh, units, kt; };     // first new row, (row, head) pairs, positions, new rows, units, tiles of 64 positions
 __device__ __forceinline__ Seq sequence(const AbsorbedParams& p, int i) {
     Seq q;
-    q.a = p.s.cu[i];
-    q.fresh = max(p.s.cu[i + 1] - q.a, 0);
+    q.a = min(max(p.s.cu[i], 0), p.s.T);
+    q.fresh = max(min(p.s.cu[i + 1], p.s.T) - q.a, 0);
     q.len = min(max(p.s.lens[i], 0), p.s.max_pages << p.s.page_shift);
     q.rows = q.fresh <= p.most ? q.fresh * p.heads : 0;
     q.units = ((q.rows + p.R - 1) / p.R + p.group - 1) / p.group;
@@ -63,41 +64,73 @@ __device__ __forceinline__ long long stretch(long long W, int groups) { return (
 
 // ---------------------------------------------------------------- queries to the latent space
 
-// A CTA: 64 latent columns of one head, up to 64 rows.  The last CTA of the grid writes the prefix sums of tiles and units instead.
-__global__ void __launch_bounds__(128) absorb_kernel(const __grid_constant__ AbsorbedParams p) {
-    pdl_launch_dependents();
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
-    const int ctiles = p.dl / 64;
-    if (blockIdx.x == gridDim.x - 1) {
-        if (blockIdx.y != 0) return;
+// Prefix sums over the sequences, and the caller's bounds: 128 threads.
+__device__ __forceinline__ void plan_sequences(const AbsorbedParams& p) {
         __shared__ long long s_t[128];
-        __shared__ int s_u[128];
-        const int per = (p.s.n + 127) / 128, i0 = min(tid * per, p.s.n), i1 = min(i0 + per, p.s.n);
+        __shared__ int s_u[128], s_r[128];
+        const int tid = threadIdx.x, per = (p.s.n + 127) / 128, i0 = min(tid * per, p.s.n), i1 = min(i0 + per, p.s.n);
         long long t = 0;
-        int u = 0;
+        int u = 0, rows = 0;
         bool ok = tid != 0 || (p.s.cu[0] == 0 && p.s.cu[p.s.n] <= p.s.T);
         for (int i = i0; i < i1; ++i) {
             const Seq q = sequence(p, i);
             t += q.units * unit_length(q);
             u += q.units;
-            ok = ok && p.s.cu[i + 1] >= q.a && q.fresh <= p.max_new && q.len >= p.s.lens[i];
+            rows += q.rows > 0 ? q.fresh : 0;
+            ok = ok && p.s.cu[i + 1] >= p.s.cu[i] && q.fresh <= p.max_new && q.len >= p.s.lens[i];
         }
         if (!ok) latent_raise(p.status, EDG_E_RANGE);
         s_t[tid] = t;
         s_u[tid] = u;
+        s_r[tid] = rows;
         __syncthreads();
         t = 0;
-        u = 0;
-        for (int j = 0; j < tid; ++j) { t += s_t[j]; u += s_u[j]; }
+        u = rows = 0;
+        for (int j = 0; j < tid; ++j) { t += s_t[j]; u += s_u[j]; rows += s_r[j]; }
         for (int i = i0; i < i1; ++i) {
             const Seq q = sequence(p, i);
             p.tile_pre[i] = t;
             p.unit_pre[i] = u;
+            p.row_pre[i] = rows;
             t += q.units * unit_length(q);
             u += q.units;
-            if (i == p.s.n - 1) { p.tile_pre[p.s.n] = t; p.unit_pre[p.s.n] = u; }
+            rows += q.rows > 0 ? q.fresh : 0;
+            if (i == p.s.n - 1) { p.tile_pre[p.s.n] = t; p.unit_pre[p.s.n] = u; p.row_pre[p.s.n] = rows; }
         }
+}
+__global__ void __launch_bounds__(128) plan_kernel(const __grid_constant__ AbsorbedParams p) {
+    pdl_launch_dependents();
+    plan_sequences(p);
+}
+
+// A CTA: 64 latent columns of one head, up to 64 rows.  Where every sequence is taken the last CTA of the grid makes the prefix sums; else
+// plan_kernel has made them, and rows are counted over the sequences that are taken.
+__global__ void __launch_bounds__(128) absorb_kernel(const __grid_constant__ AbsorbedParams p) {
+    pdl_launch_dependents();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+    const int ctiles = p.dl / 64;
+    const bool all = p.most >= p.max_new;
+    if (all && blockIdx.x == gridDim.x - 1) {
+        if (blockIdx.y == 0) plan_sequences(p);
         return;
+    }
+    __shared__ int s_row[64];                                           // new rows of this CTA, or -1
+    if (!all) {
+        pdl_wait_prior_grid();
+        const int rows = p.row_pre[p.s.n];
+        if ((int)blockIdx.y * 64 >= rows) return;
+        if (tid < 64) {
+            const int a = blockIdx.y * 64 + tid;
+            int lo = 0, hi = p.s.n;                                      // ends row_pre[1..n] that are <= a
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (p.row_pre[mid + 1] <= a) lo = mid + 1; else hi = mid;
+            }
+            s_row[tid] = lo < p.s.n ? p.s.cu[lo] + a - p.row_pre[lo] : -1;
+        }
+    } else if (tid < 64) {
+        const int a = blockIdx.y * 64 + tid;
+        s_row[tid] = a < p.s.T ? a : -1;
     }
     constexpr int kPitch = 72;                                          // elements of a row of W in shared memory: 64 and padding
     __shared__ __align__(16) uint16_t s_w[128 * kPitch];
@@ -113,25 +146,22 @@ __global__ void __launch_bounds__(128) absorb_kernel(const __grid_constant__ Abs
         for (int k = 0; k < 8; ++k)
             if (k * 16 < p.dn) *reinterpret_cast<uint4*>(s_w + (k * 16 + (tid >> 3)) * kPitch + (tid & 7) * 8) = v[k];
     }
-    const int t_end = min(p.s.T, ((int)blockIdx.y + 1) * 64);
-    if (p.most < p.max_new) {                                           // rows of one sequence that the other form takes
-        const int a = find_sequence(p.s.cu, p.s.n, blockIdx.y * 64, lane), b = find_sequence(p.s.cu, p.s.n, t_end - 1, lane);
-        if (a == b && (a == p.s.n || sequence(p, a).rows == 0)) return;
-    }
+    __syncthreads();
     if (c0 == 0)                                                        // the rotated part, zeros behind it
-        for (int i = tid; i < (t_end - (int)blockIdx.y * 64) * 8; i += 128) {
-            const int t = blockIdx.y * 64 + (i >> 3), c = (i & 7) * 8;
+        for (int i = tid; i < 64 * 8; i += 128) {
+            const int t = s_row[i >> 3], c = (i & 7) * 8;
+            if (t < 0) break;
             uint4 v = make_uint4(0, 0, 0, 0);
             if (c < p.dr) v = *reinterpret_cast<const uint4*>(p.q_rope + (size_t)t * p.ldr + h * p.hr + c);
             *reinterpret_cast<uint4*>(p.q_lat + ((size_t)t * p.heads + h) * row + p.dl + c) = v;
         }
-    __syncthreads();
     const int ks = p.dn / 16;
-    for (int t0 = blockIdx.y * 64; t0 < t_end; t0 += 16) {
+    for (int t0 = 0; t0 < 64 && s_row[t0] >= 0; t0 += 16) {
         float d[2][4] = {};
-        const bool r0 = t0 + g < t_end, r1 = t0 + g + 8 < t_end;
-        const uint16_t* q0 = p.q + (size_t)(t0 + g) * p.ldq + h * (p.dn + p.dr) + 2 * t4;
-        const uint16_t* q1 = q0 + 8 * p.ldq;
+        const int ra = s_row[t0 + g], rb = s_row[t0 + g + 8];
+        const bool r0 = ra >= 0, r1 = rb >= 0;
+        const uint16_t* q0 = p.q + (size_t)max(ra, 0) * p.ldq + h * (p.dn + p.dr) + 2 * t4;
+        const uint16_t* q1 = p.q + (size_t)max(rb, 0) * p.ldq + h * (p.dn + p.dr) + 2 * t4;
 #pragma unroll 4
         for (int k = 0; k < ks; ++k) {
             const uint32_t a0 = r0 ? *reinterpret_cast<const uint32_t*>(q0 + k * 16) : 0u, a1 = r1 ? *reinterpret_cast<const uint32_t*>(q1 + k * 16) : 0u;
@@ -145,8 +175,8 @@ __global__ void __launch_bounds__(128) absorb_kernel(const __grid_constant__ Abs
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int c = c0 + warp * 16 + j * 8 + 2 * t4;
-            if (r0) *reinterpret_cast<uint32_t*>(p.q_lat + ((size_t)(t0 + g) * p.heads + h) * row + c) = bf16_pair(d[j][0], d[j][1]);
-            if (r1) *reinterpret_cast<uint32_t*>(p.q_lat + ((size_t)(t0 + g + 8) * p.heads + h) * row + c) = bf16_pair(d[j][2], d[j][3]);
+            if (r0) *reinterpret_cast<uint32_t*>(p.q_lat + ((size_t)ra * p.heads + h) * row + c) = bf16_pair(d[j][0], d[j][1]);
+            if (r1) *reinterpret_cast<uint32_t*>(p.q_lat + ((size_t)rb * p.heads + h) * row + c) = bf16_pair(d[j][2], d[j][3]);
         }
     }
 }
@@ -315,7 +345,11 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                 int y[4];
 #pragma unroll
                 for (int b = 0; b < 4; ++b) y[b] = __shfl_sync(0xFFFFFFFFu, coord, (t * boxes - base + min(b, boxes - 1)) & 31);
-                role_wait(&r_empty[ro.slot], ro.phase ^ 1, p.status);
+                {                                                        // the places of the tile's parts, all at once: a lane looks at one
+                    RingAt at = v;
+                    for (int u = 0; u + 1 < lane && u + 1 < NU; ++u) at.next(P::NV);
+                    role_wait_all(lane == 0 ? &r_empty[ro.slot] : (lane <= NU ? &v_empty[at.slot] : nullptr), (lane == 0 ? ro.phase : at.phase) ^ 1, p.status);
+                }
                 if (half == 0 && elected()) {
                     mbar_expect_tx(&t_full[f.slot], kRope + NU * kUnit);
 #pragma unroll
@@ -324,7 +358,6 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                 }
                 ro.next(P::NR);
                 for (int u = 0; u < NU; ++u) {
-                    role_wait(&v_empty[v.slot], v.phase ^ 1, p.status);
                     if (elected()) {
 #pragma unroll
                         for (int b = 0; b < 4; ++b)
@@ -360,8 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
             q_phase ^= 1;
             for (int t = w.t0; t < w.t1; ++t, ++n) {
                 const int buf = n & 1;
-                role_wait(&s_empty[buf], ((uint32_t)(n >> 1) & 1) ^ 1, p.status);
-                role_wait(&t_full[f.slot], f.phase, p.status);
+                role_wait_all(lane == 0 ? &s_empty[buf] : (lane == 1 ? &t_full[f.slot] : nullptr), lane == 0 ? ((uint32_t)(n >> 1) & 1) ^ 1 : f.phase, p.status);
                 f.next(kFull);
                 uint32_t at[4];
 #pragma unroll
@@ -575,10 +607,15 @@ constexpr int kCombine = 512;
 __global__ void __launch_bounds__(kCombine, 1) combine_kernel(const __grid_constant__ AbsorbedParams p) {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ float s_weight[16][kSms];
-    __shared__ int s_there[16];
+    __shared__ int s_row[16];                                           // new rows of this CTA, or -1
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
     const int h = blockIdx.x, t0 = blockIdx.y * 16, pitch = p.dl * 2 + 64, kb = p.dl / 32;
     const bool values = warp * 8 < p.dv;
+    const bool all = p.most >= p.max_new;
+    if (!all) {
+        pdl_wait_prior_grid();
+        if (t0 >= p.row_pre[p.s.n]) return;
+    }
     // lane t4 of a quad takes columns 8 t4 .. 8 t4 + 7 of every 32, of both operands: any order of k will do
     uint4 w[16];
 #pragma unroll
@@ -586,11 +623,13 @@ __global__ void __launch_bounds__(kCombine, 1) combine_kernel(const __grid_const
         if (values && k < kb) w[k] = __ldg(reinterpret_cast<const uint4*>(p.W_uv + ((size_t)h * p.dv + warp * 8 + g) * p.dl + t4 * 8 + k * 32));
     pdl_wait_prior_grid();
     {
-        const int t = t0 + warp;
         int first = 0, count = 0, row = -1;
-        const int seq = t < p.s.T ? find_sequence(p.s.cu, p.s.n, t, lane) : p.s.n;
+        const int32_t* ends = all ? p.s.cu : p.row_pre;
+        const int seq = find_sequence(ends, p.s.n, t0 + warp, lane);
         const Seq q = seq < p.s.n ? sequence(p, seq) : Seq{};
-        if (q.rows > 0) {
+        const int t = q.a + t0 + warp - ends[min(seq, p.s.n)];
+        const bool there = q.rows > 0 && t < p.s.T;
+        if (there) {
             const long long W = p.tile_pre[p.s.n], before = p.tile_pre[seq];
             const int units = p.unit_pre[seq], in = (t - q.a) * p.heads + h, rt = in / p.R, ug = rt / p.group;
             row = (rt - ug * p.group) * p.R + in - rt * p.R;
@@ -622,7 +661,7 @@ __global__ void __launch_bounds__(kCombine, 1) combine_kernel(const __grid_const
                 sum = fmaf(ml[k].y, e, sum);
             }
         sum = warp_sum(sum);
-        if (lane == 0) s_there[warp] = row >= 0;
+        if (lane == 0) s_row[warp] = there ? t : -1;
         __syncwarp();
         float4 o[4];
 #pragma unroll
@@ -666,15 +705,16 @@ __global__ void __launch_bounds__(kCombine, 1) combine_kernel(const __grid_const
             }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        if (s_there[g + 8 * e] == 0) continue;
-        const size_t at = ((size_t)(t0 + g + 8 * e) * p.heads + h) * p.dv + warp * 8 + 2 * t4;
+        const int t = s_row[g + 8 * e];
+        if (t < 0) continue;
+        const size_t at = ((size_t)t * p.heads + h) * p.dv + warp * 8 + 2 * t4;
         const float x = (d[0][2 * e] + d[1][2 * e]) + (d[2][2 * e] + d[3][2 * e]), y = (d[0][2 * e + 1] + d[1][2 * e + 1]) + (d[2][2 * e + 1] + d[3][2 * e + 1]);
         if (p.out_dtype == EDG_F16) *reinterpret_cast<__half2*>(static_cast<__half*>(p.y) + at) = __floats2half2_rn(x, y);
         else *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.y) + at) = bf16_pair(x, y);
     }
 }
 
-struct AbsorbedLayout { int R, group, groups, slots; size_t tile_pre, unit_pre, q_lat, ml, part, bytes; };
+struct AbsorbedLayout { int R, group, groups, slots; size_t tile_pre, unit_pre, row_pre, q_lat, ml, part, bytes; };
 
 AbsorbedLayout absorbed_layout(const edg_latent_desc& d, int n_seqs, int T, int max_new) {
     AbsorbedLayout L;
@@ -689,7 +729,8 @@ AbsorbedLayout absorbed_layout(const edg_latent_desc& d, int n_seqs, int T, int 
     const size_t rows_all = (size_t)kSms * L.R + (size_t)(with + 1) * L.R * L.group + (size_t)all;
     L.tile_pre = kCtrlBytes;
     L.unit_pre = round_up(L.tile_pre + ((size_t)n_seqs + 1) * 8, 256);
-    L.q_lat = round_up(L.unit_pre + ((size_t)n_seqs + 1) * 4, 256);
+    L.row_pre = round_up(L.unit_pre + ((size_t)n_seqs + 1) * 4, 256);
+    L.q_lat = round_up(L.row_pre + ((size_t)n_seqs + 1) * 4, 256);
     L.ml = round_up(L.q_lat + (size_t)all * (d.d_latent + 64) * 2, 256);
     L.part = round_up(L.ml + rows_all * 8, 256);
     L.bytes = round_up(L.part + rows_all * d.d_latent * 4, 256);
@@ -718,6 +759,7 @@ int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new,
     p.ml = reinterpret_cast<float2*>(ws + L.ml);
     p.tile_pre = reinterpret_cast<long long*>(ws + L.tile_pre);
     p.unit_pre = reinterpret_cast<int32_t*>(ws + L.unit_pre);
+    p.row_pre = reinterpret_cast<int32_t*>(ws + L.row_pre);
     p.y = y;
     p.status = static_cast<int32_t*>(workspace);
     p.heads = d.heads;
@@ -746,13 +788,20 @@ int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new,
     const uint32_t kv_box[2] = {64, (uint32_t)(d.page < 64 ? d.page : 64)}, q_box[2] = {64, (uint32_t)L.R};
     EDG_CUDA_TRY(make_map(&kv_map, cache, 2, kv_dims, &row, kv_box));
     EDG_CUDA_TRY(make_map(&q_map, p.q_lat, 2, q_dims, &q_row, q_box));
-    absorb_kernel<<<dim3(d.heads * (d.d_latent / 64) + 1, (s.T + 63) / 64), 128, 0, st>>>(p);
-    EDG_CUDA_TRY(cudaGetLastError());
+    const int64_t rows = most >= max_new ? s.T : ((int64_t)s.n * most < s.T ? (int64_t)s.n * most : s.T);        // that can be taken
+    if (most >= max_new) {
+        absorb_kernel<<<dim3(d.heads * (d.d_latent / 64) + 1, (unsigned)((rows + 63) / 64)), 128, 0, st>>>(p);
+        EDG_CUDA_TRY(cudaGetLastError());
+    } else {
+        plan_kernel<<<1, 128, 0, st>>>(p);
+        EDG_CUDA_TRY(cudaGetLastError());
+        EDG_CUDA_TRY(launch_pdl(absorb_kernel, dim3(d.heads * (d.d_latent / 64), (unsigned)((rows + 63) / 64)), 128, (size_t)0, st, p));
+    }
     const dim3 grid(L.groups * L.group);
     EDG_CUDA_TRY(L.R == 16   ? launch_pdl(absorbed_kernel<16>, grid, kThreads, Plan<16>::bytes, st, p, kv_map, q_map)
                  : L.R == 32 ? launch_pdl(absorbed_kernel<32>, grid, kThreads, Plan<32>::bytes, st, p, kv_map, q_map)
                              : launch_pdl(absorbed_kernel<64>, grid, kThreads, Plan<64>::bytes, st, p, kv_map, q_map));
-    EDG_CUDA_TRY(launch_pdl(combine_kernel, dim3(d.heads, (s.T + 15) / 16), kCombine, (size_t)32 * (d.d_latent * 2 + 64), st, p));
+    EDG_CUDA_TRY(launch_pdl(combine_kernel, dim3(d.heads, (unsigned)((rows + 15) / 16)), kCombine, (size_t)32 * (d.d_latent * 2 + 64), st, p));
     return EDG_OK;
 }
 

@@ -36,7 +36,7 @@ namespace {
 struct XSeq { int a, fresh, len, pairs, tiles; };
 __device__ __forceinline__ XSeq xsequence(const ExpandedParams& p, int i) {
     XSeq q;
-    q.a = p.s.cu[i];
+    q.a = min(max(p.s.cu[i], 0), p.s.T);
     q.fresh = max(min(p.s.cu[i + 1], p.s.T) - q.a, 0);
     q.len = min(max(p.s.lens[i], 0), p.s.max_pages << p.s.page_shift);
     const bool mine = q.fresh > p.more_than;
@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(256) prompt_plan_kernel(const __grid_constant_
         q += x.pairs;
         k += x.tiles;
         len += x.len;
-        ok = ok && p.s.cu[i + 1] >= x.a && p.s.cu[i + 1] - x.a <= p.max_new && x.len >= p.s.lens[i];
+        ok = ok && p.s.cu[i + 1] >= p.s.cu[i] && x.fresh <= p.max_new && x.len >= p.s.lens[i];
     }
     s_q[tid] = q;
     s_k[tid] = k;
@@ -86,9 +86,9 @@ __global__ void __launch_bounds__(256) prompt_plan_kernel(const __grid_constant_
 // ---------------------------------------------------------------- keys and values
 
 constexpr int kXThreads = 256;              // warp 0 loads, warp 1 issues products, warps 4-7 write out
-constexpr int kXRing = 5;
+constexpr int kXRing = 3;                   // stages of 128 columns: with one chunk a stage, waits took as long as products
 constexpr uint32_t kChunk = 16384;          // 128 rows of 64 columns
-constexpr uint32_t kXW = 8 * kChunk, kXBars = kXW + kXRing * kChunk, kXBytes = kXBars + 256 + 1024;
+constexpr uint32_t kXW = 8 * kChunk, kXBars = kXW + kXRing * 2 * kChunk, kXBytes = kXBars + 256 + 1024;
 
 __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_constant__ ExpandedParams p, const __grid_constant__ CUtensorMap c_map,
                                                               const __grid_constant__ CUtensorMap uk_map, const __grid_constant__ CUtensorMap uv_map) {
@@ -143,12 +143,13 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
             RingAt w;
             for (int h = h0; h < h1; ++h)
                 for (int kv = 0; kv < 2; ++kv)
-                    for (int c = 0; c < nc; ++c) {
+                    for (int c = 0; c < nc; c += 2) {
                         role_wait(&w_empty[w.slot], w.phase ^ 1, p.status);
                         if (elected()) {
                             const int n = kv == 0 ? p.dn : p.dv;
-                            tma_2d(sb + kXW + w.slot * kChunk, kv == 0 ? &uk_map : &uv_map, c * 64, h * n, &w_full[w.slot]);
-                            mbar_expect_tx(&w_full[w.slot], n * 128);
+                            tma_2d(sb + kXW + w.slot * 2 * kChunk, kv == 0 ? &uk_map : &uv_map, c * 64, h * n, &w_full[w.slot]);
+                            tma_2d(sb + kXW + w.slot * 2 * kChunk + kChunk, kv == 0 ? &uk_map : &uv_map, c * 64 + 64, h * n, &w_full[w.slot]);
+                            mbar_expect_tx(&w_full[w.slot], n * 256);
                         }
                         __syncwarp();
                         w.next(kXRing);
@@ -162,15 +163,16 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
                 for (int kv = 0; kv < 2; ++kv, ++j) {
                     const uint32_t id = idesc_bf16(128, kv == 0 ? p.dn : p.dv), d = tmem + (j & 1) * 128;
                     role_wait(&d_empty[j & 1], ((uint32_t)(j >> 1) & 1) ^ 1, p.status);
-                    for (int c = 0; c < nc; ++c) {
+                    for (int c = 0; c < nc; c += 2) {
                         role_wait(&w_full[w.slot], w.phase, p.status);
                         tc_fence_after();
                         if (elected()) {
 #pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                umma_ss(d, dc + ((c * kChunk + k * 32) >> 4), dw + ((w.slot * kChunk + k * 32) >> 4), id, c + k > 0);
+                            for (int k = 0; k < 8; ++k)
+                                umma_ss(d, dc + (((c + (k >> 2)) * kChunk + (k & 3) * 32) >> 4), dw + ((w.slot * 2 * kChunk + (k >> 2) * kChunk + (k & 3) * 32) >> 4), id,
+                                        c + k > 0);
                             umma_done(&w_empty[w.slot]);
-                            if (c == nc - 1) umma_done(&d_full[j & 1]);
+                            if (c == nc - 2) umma_done(&d_full[j & 1]);
                         }
                         __syncwarp();
                         w.next(kXRing);
@@ -236,14 +238,14 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
     uint64_t* kv_full = empty + kPRing;                                  // [kPRing] keys of a tile, its values, the next keys ...: never more than chunks
     uint64_t* q_full = kv_full + kPRing;                                      // [2]
     uint64_t* s_full = q_full + 2;                                       // [2]
-    uint64_t* p_full = s_full + 2;                                       // [2]
-    uint64_t* o_done = p_full + 2;                                       // [2]
+    uint64_t* p_full = s_full + 2;                                       // [2][2] halves of P
+    uint64_t* o_done = p_full + 4;                                       // [2]
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(o_done + 2);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         for (int i = 0; i < kPRing; ++i) mbar_init(&empty[i], 1);
         for (int i = 0; i < kPRing; ++i) mbar_init(&kv_full[i], 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&q_full[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); mbar_init(&o_done[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&q_full[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[2 * i], 4); mbar_init(&p_full[2 * i + 1], 4); mbar_init(&o_done[i], 1); }
         fence_barrier_init();
     }
     if (warp == 1) tmem_alloc(s_tmem, 512);
@@ -268,7 +270,113 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
         }
         const int nt = max(n[0], n[1]);
         const int nkc = (p.dn + 63) / 64, nvc = (p.dv + 63) / 64;        // chunks of keys (and one of rotated parts), of values
-        if (warp == 0) {
+        // (registers: 128 threads of 80 and 256 of 208 are 63488, of the launch's 384 x 168 = 64512)
+        if (warp >= 4) {
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+            // ========================================= softmax: a thread is a row
+            const int i = (warp >> 2) - 1, wq = warp & 3, row = i * 128 + wq * 32 + lane;
+            const uint32_t st = tmem + ((uint32_t)(wq * 32) << 16) + i * 128, ot = st + 256;
+            const float k2 = p.scale * 1.4426950408889634f;
+            const int pos = pos0 + row;                                  // positions 0 .. pos are seen
+            float m = -INFINITY, l = 0.f;
+            const int mine = i == 0 ? n[0] : n[1];
+            for (int t = 0; t < mine; ++t) {
+                role_wait(&s_full[i], (uint32_t)t & 1, p.status);
+                tc_fence_after();
+                const int seen = pos + 1 - t * 128;                      // of this tile
+                const bool part = __any_sync(0xFFFFFFFFu, seen < 128);
+                // 128 scores of the row in registers, the largest of them
+                uint32_t v[2][64];
+                float mt;
+                {
+                    float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        tmem_ld(st + x * 64, v[x]);
+                        if (part) {
+#pragma unroll
+                            for (int j = 0; j < 64; ++j)
+                                if (x * 64 + j >= seen) v[x][j] = 0xFF800000u;
+                        }
+#pragma unroll
+                        for (int j = 0; j < 64; j += 8)
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) a[y] = max3(a[y], __uint_as_float(v[x][j + y]), __uint_as_float(v[x][j + 4 + y]));
+                    }
+                    mt = fmaxf(m, fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])) * k2);         // (the scale is positive)
+                }
+                if (t == 0) m = mt;
+                const bool grown = mt > m + 8.f;
+                if (__any_sync(0xFFFFFFFFu, grown)) {
+                    const float alpha = grown ? exp2_approx(m - mt) : 1.f;
+                    if (grown) { m = mt; l *= alpha; }
+                    role_wait(&o_done[i], (uint32_t)(t - 1) & 1, p.status);
+                    tc_fence_after();
+                    for (int c = 0; c < p.dv; c += 16) {
+                        uint32_t o[16];
+                        tmem_ld(ot + c, o);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                        tmem_st(ot + c, o);
+                    }
+                    tmem_st_wait();
+                }
+                const float mm = m == -INFINITY ? 0.f : -m;
+                const float2 k22 = make_float2(k2, k2), mm2 = make_float2(mm, mm);
+                float2 sum = make_float2(0.f, 0.f);
+                // P of the first 64 positions goes to the tensor cores while that of the others is made
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+#pragma unroll
+                    for (int c = 0; c < 64; c += 32) {
+                        uint32_t o[16];
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) {
+                            const float2 e = fma_2(make_float2(__uint_as_float(v[x][c + j]), __uint_as_float(v[x][c + j + 1])), k22, mm2);
+                            const float2 w = make_float2(exp2_approx(e.x), exp2_approx(e.y));
+                            sum = add_2(sum, w);
+                            o[j / 2] = bf16_pair(w.x, w.y);
+                        }
+                        tmem_st(st + x * 32 + c / 2, o);                 // (over scores that have been read)
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_full[2 * i + x]);
+                }
+                l += sum.x + sum.y;
+            }
+            // ---- out
+            const bool have = r0 + row < q.fresh && fits;
+            if (mine > 0) {
+                role_wait(&o_done[i], (uint32_t)(mine - 1) & 1, p.status);
+                tc_fence_after();
+            }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const size_t out = ((size_t)(q.a + r0 + row) * p.heads + h) * p.dv;
+            for (int c = 0; c < p.dv; c += 16) {
+                uint32_t v[16], o[8];
+                if (mine > 0) tmem_ld(ot + c, v);
+                else
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[j] = 0u;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float a = l == 0.f ? 0.f : __uint_as_float(v[2 * j]) * inv, b = l == 0.f ? 0.f : __uint_as_float(v[2 * j + 1]) * inv;
+                    if (p.out_dtype == EDG_F16) {
+                        const __half2 x = __floats2half2_rn(a, b);
+                        o[j] = *reinterpret_cast<const uint32_t*>(&x);
+                    } else o[j] = bf16_pair(a, b);
+                }
+                if (have) {
+                    uint4* y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y) + out + c);
+                    y[0] = make_uint4(o[0], o[1], o[2], o[3]);
+                    y[1] = make_uint4(o[4], o[5], o[6], o[7]);
+                }
+            }
+        } else {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+            if (warp == 0) {
             // ========================================= loads
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -310,7 +418,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
             const int rks = p.dr / 16;
             RingAt f;                                                    // the next group (keys or values) to wait for
             int at = 0;                                                  // ring place of the next group
-            auto take = [&](int chunks) { const int a = at; at = (at + chunks) & (kPRing - 1); role_wait(&kv_full[f.slot], f.phase, p.status); f.next(kPRing); return a; };
+            auto take = [&](int chunks) { const int a = at; at = (at + chunks) & (kPRing - 1); return a; };
             auto scores = [&](int i, int k) {
                 if (elected()) {
                     for (int c = 0; c < nkc; ++c) {
@@ -334,6 +442,8 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
             int k = 0;
             if (nt > 0) {
                 k = take(nkc + 1);
+                role_wait(&kv_full[f.slot], f.phase, p.status);
+                f.next(kPRing);
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     if (n[i] > 0) {
@@ -345,141 +455,44 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
             }
             for (int t = 0; t < nt; ++t) {
                 const int v = take(nvc);
-                if (t + 1 < nt) k = take(nkc + 1);
+                {                                                        // this tile's values and the next one's keys
+                    const RingAt a = f;
+                    f.next(kPRing);
+                    const bool more = t + 1 < nt;
+                    role_wait_all(lane == 0 ? &kv_full[a.slot] : (lane == 1 && more ? &kv_full[f.slot] : nullptr), lane == 0 ? a.phase : f.phase, p.status);
+                    if (more) { f.next(kPRing); k = take(nkc + 1); }
+                }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     if (t < n[i]) {
-                        role_wait(&p_full[i], (uint32_t)t & 1, p.status);
-                        tc_fence_after();
-                        if (elected()) {
-                            const bool whole = nvc == 1 || v + 1 < kPRing;     // (values that go round the ring's end: a chunk at a time)
-                            const uint32_t b = dv + ((v * kChunk) >> 4);
-                            const uint32_t o = tmem + 256 + i * 128, pt = tmem + i * 128;
-                            if (whole) {
+                        const bool whole = nvc == 1 || v + 1 < kPRing;         // (values that go round the ring's end: a chunk at a time)
+                        const uint32_t b = dv + ((v * kChunk) >> 4), o = tmem + 256 + i * 128, pt = tmem + i * 128;
 #pragma unroll
-                                for (int s = 0; s < 8; ++s) umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id_o, t > 0 || s > 0);
-                            } else {
-                                const uint32_t id0 = idesc_bf16(128, 64, false, true), id1 = idesc_bf16(128, p.dv - 64, false, true);
+                        for (int half = 0; half < 2; ++half) {
+                            role_wait(&p_full[2 * i + half], (uint32_t)t & 1, p.status);
+                            tc_fence_after();
+                            if (elected()) {
+                                if (whole) {
 #pragma unroll
-                                for (int s = 0; s < 8; ++s) {
-                                    umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id0, t > 0 || s > 0);
-                                    umma_ts(o + 64, pt + s * 8, dv + ((s * 2048) >> 4), id1, t > 0 || s > 0);
+                                    for (int s = half * 4; s < half * 4 + 4; ++s) umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id_o, t > 0 || s > 0);
+                                } else {
+                                    const uint32_t id0 = idesc_bf16(128, 64, false, true), id1 = idesc_bf16(128, p.dv - 64, false, true);
+#pragma unroll
+                                    for (int s = half * 4; s < half * 4 + 4; ++s) {
+                                        umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id0, t > 0 || s > 0);
+                                        umma_ts(o + 64, pt + s * 8, dv + ((s * 2048) >> 4), id1, t > 0 || s > 0);
+                                    }
                                 }
+                                if (half == 1) umma_done(&o_done[i]);
                             }
-                            umma_done(&o_done[i]);
+                            __syncwarp();
                         }
-                        __syncwarp();
                     }
                     if (t + 1 < n[i]) scores(i, k);
                 }
                 release(v, nvc);
                 if (t + 1 < nt) release(k, nkc + 1);
             }
-        } else if (warp >= 4) {
-            // ========================================= softmax: a thread is a row
-            const int i = (warp >> 2) - 1, wq = warp & 3, row = i * 128 + wq * 32 + lane;
-            const uint32_t st = tmem + ((uint32_t)(wq * 32) << 16) + i * 128, ot = st + 256;
-            const float k2 = p.scale * 1.4426950408889634f;
-            const int pos = pos0 + row;                                  // positions 0 .. pos are seen
-            float m = -INFINITY, l = 0.f;
-            const int mine = i == 0 ? n[0] : n[1];
-            for (int t = 0; t < mine; ++t) {
-                role_wait(&s_full[i], (uint32_t)t & 1, p.status);
-                tc_fence_after();
-                const int seen = pos + 1 - t * 128;                      // of this tile
-                const bool part = __any_sync(0xFFFFFFFFu, seen < 128);
-                float mt = m;
-#pragma unroll
-                for (int c = 0; c < 128; c += 32) {
-                    uint32_t v[32];
-                    tmem_ld(st + c, v);
-                    if (part) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (c + j >= seen) v[j] = 0xFF800000u;
-                    }
-                    float a = -INFINITY, b = -INFINITY, d = -INFINITY, e = -INFINITY;
-                    if (k2 >= 0.f) {
-#pragma unroll
-                        for (int j = 0; j < 32; j += 4) {
-                            a = fmaxf(a, __uint_as_float(v[j])); b = fmaxf(b, __uint_as_float(v[j + 1]));
-                            d = fmaxf(d, __uint_as_float(v[j + 2])); e = fmaxf(e, __uint_as_float(v[j + 3]));
-                        }
-                        a = fmaxf(fmaxf(a, b), fmaxf(d, e));
-                        if (a != -INFINITY) mt = fmaxf(mt, a * k2);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (!part || c + j < seen) mt = fmaxf(mt, __uint_as_float(v[j]) * k2);
-                    }
-                }
-                if (t == 0) m = mt;
-                const bool grown = mt > m + 8.f;
-                if (__any_sync(0xFFFFFFFFu, grown)) {
-                    const float alpha = grown ? exp2_approx(m - mt) : 1.f;
-                    if (grown) { m = mt; l *= alpha; }
-                    role_wait(&o_done[i], (uint32_t)(t - 1) & 1, p.status);
-                    tc_fence_after();
-                    for (int c = 0; c < p.dv; c += 16) {
-                        uint32_t v[16];
-                        tmem_ld(ot + c, v);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * alpha);
-                        tmem_st(ot + c, v);
-                    }
-                }
-                const float mm = m == -INFINITY ? 0.f : m;
-#pragma unroll
-                for (int c = 0; c < 128; c += 32) {
-                    uint32_t v[32], o[16];
-                    tmem_ld(st + c, v);
-                    float la = 0.f, lb = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        float a = exp2_approx(fmaf(__uint_as_float(v[j]), k2, -mm)), b = exp2_approx(fmaf(__uint_as_float(v[j + 1]), k2, -mm));
-                        if (part) {
-                            if (c + j >= seen) a = 0.f;
-                            if (c + j + 1 >= seen) b = 0.f;
-                        }
-                        o[j / 2] = bf16_pair(a, b);
-                        la += a;
-                        lb += b;
-                    }
-                    l += la + lb;
-                    tmem_st(st + c / 2, o);                              // (over columns that have been read)
-                }
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[i]);
-            }
-            // ---- out
-            const bool have = r0 + row < q.fresh && fits;
-            if (mine > 0) {
-                role_wait(&o_done[i], (uint32_t)(mine - 1) & 1, p.status);
-                tc_fence_after();
-            }
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            const size_t out = ((size_t)(q.a + r0 + row) * p.heads + h) * p.dv;
-            for (int c = 0; c < p.dv; c += 16) {
-                uint32_t v[16], o[8];
-                if (mine > 0) tmem_ld(ot + c, v);
-                else
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] = 0u;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float a = l == 0.f ? 0.f : __uint_as_float(v[2 * j]) * inv, b = l == 0.f ? 0.f : __uint_as_float(v[2 * j + 1]) * inv;
-                    if (p.out_dtype == EDG_F16) {
-                        const __half2 x = __floats2half2_rn(a, b);
-                        o[j] = *reinterpret_cast<const uint32_t*>(&x);
-                    } else o[j] = bf16_pair(a, b);
-                }
-                if (have) {
-                    uint4* y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y) + out + c);
-                    y[0] = make_uint4(o[0], o[1], o[2], o[3]);
-                    y[1] = make_uint4(o[4], o[5], o[6], o[7]);
-                }
             }
         }
     }
@@ -533,9 +546,13 @@ int32_t run_expanded(const edg_latent_desc& d, const LatentSeqs& s, int max_new,
     p.max_new = max_new;
     p.total_len = total_len;
     p.scale = d.scale;
-    // heads of a tile of positions are shared out until there is a CTA for every SM
-    const int tiles = L.rows / 128;
-    p.splits = 148 / tiles < 1 ? 1 : (148 / tiles > d.heads ? d.heads : 148 / tiles);
+    // the heads of a tile of positions are shared out so that the CTAs' rounds take the least, a CTA's start counted as a head
+    const int64_t tiles = L.rows / 128;
+    int64_t least = 0;
+    for (int x = 1; x <= d.heads; ++x) {
+        const int64_t cost = (tiles * x + 147) / 148 * ((d.heads + x - 1) / x + 1);
+        if (x == 1 || cost < least) { least = cost; p.splits = x; }
+    }
     static OncePerDevice once;
     EDG_CUDA_TRY(once([] {
         const cudaError_t e = allow_smem(kXBytes, expand_kernel);
@@ -582,7 +599,7 @@ int32_t run_expanded(const edg_latent_desc& d, const LatentSeqs& s, int max_new,
     }
     prompt_plan_kernel<<<1, 256, 0, st>>>(p);
     EDG_CUDA_TRY(cudaGetLastError());
-    EDG_CUDA_TRY(launch_pdl(expand_kernel, dim3(tiles, p.splits), kXThreads, kXBytes, st, p, c_map, uk_map, uv_map));
+    EDG_CUDA_TRY(launch_pdl(expand_kernel, dim3((unsigned)tiles, p.splits), kXThreads, kXBytes, st, p, c_map, uk_map, uv_map));
     const int with = s.n < s.T ? s.n : s.T;
     EDG_CUDA_TRY(launch_pdl(prompt_kernel, dim3(d.heads * (s.T / 256 + with)), kPThreads, kPBytes, st, p, qn_map, qr_map, k_map, r_map, v_map));
     return EDG_OK;

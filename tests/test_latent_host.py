@@ -22,7 +22,7 @@ def _desc(edg, **kw):
                                      (dict(d_rope=80), -2), (dict(d_rope=40), -2), (dict(d_v=136), -2), (dict(d_latent=64), -2), (dict(d_latent=320), -2),
                                      (dict(d_latent=640), -2), (dict(page=8), -2), (dict(page=48), -2), (dict(page=512), -2), (dict(n_pages=0), -2),
                                      (dict(n_pages=2 ** 25), -2), (dict(max_pages=0), -2), (dict(max_pages=2 ** 26), -2), (dict(out_dtype="f32"), -1),
-                                     (dict(form=3), -1), (dict(ldkv=280), -2), (dict(ldkv=290), -2), (dict(ldq=760), -2), (dict(ldq=770), -2)])
+                                     (dict(form=3), -1), (dict(scale=0.0), -1), (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(ldkv=280), -2), (dict(ldkv=290), -2), (dict(ldq=760), -2), (dict(ldq=770), -2)])
 def test_descriptors_that_are_refused(edg, kw, code):
     with pytest.raises(edg.EdgError) as e:
         edg.latent_workspace_bytes(_desc(edg, **kw), 1, 1, 1, 1)
