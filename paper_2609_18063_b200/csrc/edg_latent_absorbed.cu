@@ -560,6 +560,21 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                         c.next(P::NV);
                     }
                 }
+                // Of the new rows themselves some see less than others: one that is not finite is NaN by its score for those that see it, and
+                // must not reach the others by their weight of zero.
+                const int own = max(w.q.len - w.q.fresh + 1 - t * 64, 0);
+                if (own < min(held, 64))
+                    for (int i = own + wq; i < min(held, 64); i += 4) {
+                        uint32_t most = 0;
+                        RingAt c = vt;
+                        for (int u = 0; u < NU; ++u, c.next(P::NV))
+                            if (lane < 16) most = bf16_magnitudes(most, *reinterpret_cast<const uint4*>(smem + P::unit + c.slot * kUnit + (lane >> 3) * kRope + i * 128 + (lane & 7) * 16));
+                        if (__any_sync(0xFFFFFFFFu, bf16_not_finite(most))) {
+                            c = vt;
+                            for (int u = 0; u < NU; ++u, c.next(P::NV))
+                                if (lane < 16) *reinterpret_cast<uint4*>(smem + P::unit + c.slot * kUnit + (lane >> 3) * kRope + i * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                    }
                 for (int u = 0; u < NU; ++u) vt.next(P::NV);
                 fence_proxy_async();
                 __syncwarp();

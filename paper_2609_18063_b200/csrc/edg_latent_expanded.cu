@@ -182,6 +182,14 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
             const int wq = warp & 3, row = wq * 32 + lane;
             const uint32_t lanes = (uint32_t)(wq * 32) << 16;
             const bool held = pos0 + row < q.len;
+            // A cache row that is not finite makes its scores NaN for all that see it; its values are zeros, so that rows that do not see
+            // it stay what they are (their weight of zero times NaN would not).
+            uint32_t most = 0;
+            role_wait(c_full, 0, p.status);
+            for (int c = 0; c < nc; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) most = bf16_magnitudes(most, *reinterpret_cast<const uint4*>(smem + c * kChunk + row * 128 + j * 16));
+            const bool finite = !bf16_not_finite(most);
             if (split == 0) {                                            // the rotated part of this thread's row
                 uint4* out = reinterpret_cast<uint4*>(p.Rp + ((size_t)tile * 128 + row) * 64);
                 const int at = pos0 + row;
@@ -197,6 +205,7 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
             for (int h = h0; h < h1; ++h)
                 for (int kv = 0; kv < 2; ++kv, ++j) {
                     const int n = kv == 0 ? p.dn : p.dv;
+                    const bool keep = held && (kv == 0 || finite);
                     uint16_t* out = (kv == 0 ? p.K : p.V) + ((size_t)h * p.rows + (size_t)tile * 128 + row) * n;
                     role_wait(&d_full[j & 1], (uint32_t)(j >> 1) & 1, p.status);
                     tc_fence_after();
@@ -206,7 +215,7 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
                         tmem_ld(tmem + lanes + (j & 1) * 128 + c, v);
                         uint32_t o[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) o[i] = held ? bf16_pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])) : 0u;
+                        for (int i = 0; i < 8; ++i) o[i] = keep ? bf16_pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])) : 0u;
                         *reinterpret_cast<uint4*>(out + c) = make_uint4(o[0], o[1], o[2], o[3]);
                         *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(o[4], o[5], o[6], o[7]);
                     }
@@ -226,6 +235,7 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
 
 constexpr int kPThreads = 384;              // warp 0 loads, warp 1 issues products, warps 4-7 and 8-11 a tile of rows each
 constexpr int kPRing = 8;
+constexpr int kCubicOf = 8, kCubic = 2;     // of 8 weights, 2 are made on the multipliers
 constexpr uint32_t kPQ = 0, kPRingAt = 6 * kChunk, kPBars = kPRingAt + kPRing * kChunk, kPBytes = kPBars + 512 + 1024;
 
 __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_constant__ ExpandedParams p, const __grid_constant__ CUtensorMap qn_map,
@@ -234,8 +244,8 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     const uint32_t sb = smem_u32(smem);
-    uint64_t* empty = reinterpret_cast<uint64_t*>(smem + kPBars);        // [kPRing] chunks that may be overwritten
-    uint64_t* kv_full = empty + kPRing;                                  // [kPRing] keys of a tile, its values, the next keys ...: never more than chunks
+    uint64_t* kv_empty = reinterpret_cast<uint64_t*>(smem + kPBars);     // [kPRing] the groups below, read
+    uint64_t* kv_full = kv_empty + kPRing;                                  // [kPRing] keys of a tile, its values, the next keys ...: never more than chunks
     uint64_t* q_full = kv_full + kPRing;                                      // [2]
     uint64_t* s_full = q_full + 2;                                       // [2]
     uint64_t* p_full = s_full + 2;                                       // [2][2] halves of P
@@ -243,7 +253,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(o_done + 2);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (int i = 0; i < kPRing; ++i) mbar_init(&empty[i], 1);
+        for (int i = 0; i < kPRing; ++i) mbar_init(&kv_empty[i], 1);
         for (int i = 0; i < kPRing; ++i) mbar_init(&kv_full[i], 1);
         for (int i = 0; i < 2; ++i) { mbar_init(&q_full[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[2 * i], 4); mbar_init(&p_full[2 * i + 1], 4); mbar_init(&o_done[i], 1); }
         fence_barrier_init();
@@ -303,7 +313,9 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
 #pragma unroll
                             for (int y = 0; y < 4; ++y) a[y] = max3(a[y], __uint_as_float(v[x][j + y]), __uint_as_float(v[x][j + 4 + y]));
                     }
-                    mt = fmaxf(m, fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])) * k2);         // (the scale is positive)
+                    mt = max3(max3(a[0], a[1], a[2]), a[3], a[3]) * k2;  // (the scale is positive)
+                    if (!(mt < INFINITY)) { l = __int_as_float(0x7FFFFFFF); mt = -INFINITY; }      // NaN or infinity among them: so is the row
+                    mt = fmaxf(m, mt);
                 }
                 if (t == 0) m = mt;
                 const bool grown = mt > m + 8.f;
@@ -333,7 +345,13 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
 #pragma unroll
                         for (int j = 0; j < 32; j += 2) {
                             const float2 e = fma_2(make_float2(__uint_as_float(v[x][c + j]), __uint_as_float(v[x][c + j + 1])), k22, mm2);
-                            const float2 w = make_float2(exp2_approx(e.x), exp2_approx(e.y));
+                            float2 w;                                    // (every fourth pair on the multipliers)
+                            if (j % kCubicOf < kCubic) w = exp2_cubic(e);
+                            else w = make_float2(exp2_approx(e.x), exp2_approx(e.y));
+                            if (part) {
+                                if (x * 64 + c + j >= seen) w.x = 0.f;
+                                if (x * 64 + c + j + 1 >= seen) w.y = 0.f;
+                            }
                             sum = add_2(sum, w);
                             o[j / 2] = bf16_pair(w.x, w.y);
                         }
@@ -386,29 +404,38 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                     tma_3d(sb + kPQ + (i * 3 + nkc) * kChunk, &qr_map, 0, h, q.a + r0 + i * 128, &q_full[i]);
                 }
             __syncwarp();
-            RingAt w, f;
+            // Groups (the keys of a tile, its values, the next keys ...) take the ring's chunks in turn and are read in that order: a group waits
+            // until those before it have left it room.
+            RingAt f, old;
+            int at = 0, held = 0;                                        // place of the next chunk; chunks that have not been read
+            bool old_keys = true;
+            auto room = [&](int chunks) {
+                held += chunks;
+                while (held > kPRing) {
+                    role_wait(&kv_empty[old.slot], old.phase, p.status);
+                    held -= old_keys ? nkc + 1 : nvc;
+                    old_keys = !old_keys;
+                    old.next(kPRing);
+                }
+            };
             for (int t = 0; t < nt; ++t) {
                 const int row = kv0 + t * 128;
-                for (int c = 0; c <= nkc; ++c) {
-                    role_wait(&empty[w.slot], w.phase ^ 1, p.status);
-                    if (elected()) {
-                        if (c == 0) mbar_expect_tx(&kv_full[f.slot], (nkc + 1) * kChunk);
-                        if (c < nkc) tma_3d(sb + kPRingAt + w.slot * kChunk, &k_map, c * 64, row, h, &kv_full[f.slot]);
-                        else tma_2d(sb + kPRingAt + w.slot * kChunk, &r_map, 0, row, &kv_full[f.slot]);
-                    }
-                    __syncwarp();
-                    w.next(kPRing);
+                room(nkc + 1);
+                if (elected()) {
+                    mbar_expect_tx(&kv_full[f.slot], (nkc + 1) * kChunk);
+                    for (int c = 0; c < nkc; ++c) tma_3d(sb + kPRingAt + ((at + c) & (kPRing - 1)) * kChunk, &k_map, c * 64, row, h, &kv_full[f.slot]);
+                    tma_2d(sb + kPRingAt + ((at + nkc) & (kPRing - 1)) * kChunk, &r_map, 0, row, &kv_full[f.slot]);
                 }
+                __syncwarp();
+                at = (at + nkc + 1) & (kPRing - 1);
                 f.next(kPRing);
-                for (int c = 0; c < nvc; ++c) {
-                    role_wait(&empty[w.slot], w.phase ^ 1, p.status);
-                    if (elected()) {
-                        if (c == 0) mbar_expect_tx(&kv_full[f.slot], nvc * kChunk);
-                        tma_3d(sb + kPRingAt + w.slot * kChunk, &v_map, c * 64, row, h, &kv_full[f.slot]);
-                    }
-                    __syncwarp();
-                    w.next(kPRing);
+                room(nvc);
+                if (elected()) {
+                    mbar_expect_tx(&kv_full[f.slot], nvc * kChunk);
+                    for (int c = 0; c < nvc; ++c) tma_3d(sb + kPRingAt + ((at + c) & (kPRing - 1)) * kChunk, &v_map, c * 64, row, h, &kv_full[f.slot]);
                 }
+                __syncwarp();
+                at = (at + nvc) & (kPRing - 1);
                 f.next(kPRing);
             }
         } else if (warp == 1) {
@@ -434,10 +461,11 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                 }
                 __syncwarp();
             };
-            auto release = [&](int k, int chunks) {
-                if (elected())
-                    for (int c = 0; c < chunks; ++c) umma_done(&empty[(k + c) & (kPRing - 1)]);
+            int read = 0;                                                // groups
+            auto release = [&]() {
+                if (elected()) umma_done(&kv_empty[read & (kPRing - 1)]);
                 __syncwarp();
+                ++read;
             };
             int k = 0;
             if (nt > 0) {
@@ -451,17 +479,13 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                         tc_fence_after();
                         scores(i, k);
                     }
-                release(k, nkc + 1);
+                release();
             }
             for (int t = 0; t < nt; ++t) {
                 const int v = take(nvc);
-                {                                                        // this tile's values and the next one's keys
-                    const RingAt a = f;
-                    f.next(kPRing);
-                    const bool more = t + 1 < nt;
-                    role_wait_all(lane == 0 ? &kv_full[a.slot] : (lane == 1 && more ? &kv_full[f.slot] : nullptr), lane == 0 ? a.phase : f.phase, p.status);
-                    if (more) { f.next(kPRing); k = take(nkc + 1); }
-                }
+                role_wait(&kv_full[f.slot], f.phase, p.status);
+                f.next(kPRing);
+                bool next_keys = false;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     if (t < n[i]) {
@@ -488,10 +512,19 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                             __syncwarp();
                         }
                     }
-                    if (t + 1 < n[i]) scores(i, k);
+                    if (i == 1) release();                               // (the values)
+                    if (t + 1 < n[i]) {
+                        if (!next_keys) {
+                            k = take(nkc + 1);
+                            role_wait(&kv_full[f.slot], f.phase, p.status);
+                            tc_fence_after();
+                            f.next(kPRing);
+                            next_keys = true;
+                        }
+                        scores(i, k);
+                    }
                 }
-                release(v, nvc);
-                if (t + 1 < nt) release(k, nkc + 1);
+                if (next_keys) release();
             }
             }
         }

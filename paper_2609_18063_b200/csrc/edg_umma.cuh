@@ -132,10 +132,10 @@ __device__ __forceinline__ float exp2_approx(float v) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-// the larger of three; two values of a * b + c, and of a + b, in one instruction
+// the largest of three, NaN if one of them is; two values of a * b + c, and of a + b, in one instruction
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
 __device__ __forceinline__ float2 fma_2(float2 a, float2 b, float2 c) {
@@ -150,6 +150,27 @@ __device__ __forceinline__ float2 add_2(float2 a, float2 b) {
         : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
+// 2^x of two values on the multipliers, for what the unit of ex2 has no time for: x is split into an integer and a rest in [-1/2, 1/2] (Cody and
+// Waite's reduction, by the rounding of an addition), 2^rest is a cubic (minimax of the relative error, 7.5e-5, by Remez exchange), the integer
+// goes into the exponent.  x <= 127; below -126 it counts as -126.
+__device__ __forceinline__ float2 exp2_cubic(float2 x) {
+    x.x = fmaxf(x.x, -126.f);
+    x.y = fmaxf(x.y, -126.f);
+    const float2 big = make_float2(12582912.f, 12582912.f), t = add_2(x, big);
+    const float2 f = add_2(x, make_float2(12582912.f - t.x, 12582912.f - t.y));
+    float2 p = fma_2(make_float2(0.0551716685f, 0.0551716685f), f, make_float2(0.2426111251f, 0.2426111251f));
+    p = fma_2(p, f, make_float2(0.6932609677f, 0.6932609677f));
+    p = fma_2(p, f, make_float2(0.9999280572f, 0.9999280572f));
+    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+}
+// the largest magnitudes so far of the bf16 values of 16 bytes, as bits; whether one of them is infinite or NaN
+__device__ __forceinline__ uint32_t bf16_magnitudes(uint32_t m, uint4 v) {
+    m = __vmaxu2(m, v.x & 0x7FFF7FFFu);
+    m = __vmaxu2(m, v.y & 0x7FFF7FFFu);
+    m = __vmaxu2(m, v.z & 0x7FFF7FFFu);
+    return __vmaxu2(m, v.w & 0x7FFF7FFFu);
+}
+__device__ __forceinline__ bool bf16_not_finite(uint32_t m) { return (m & 0xFFFFu) >= 0x7F80u || (m >> 16) >= 0x7F80u; }
 // two fp32 -> packed bf16, a in the low half
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
     uint32_t r;

@@ -175,6 +175,26 @@ def test_a_row_of_the_cache_that_is_not_finite_reaches_its_sequence_alone(form):
 
 
 @pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("new,length,where", [(5, 70, 67), (40, 40, 0), (40, 100, 99), (140, 300, 200), (150, 150, 127), (300, 300, 131)])
+def test_a_new_row_that_is_not_finite_reaches_no_row_before_it(form, value, new, length, where):
+    b = Batch(SMALL, [new, 1], [length, 50], form=form)
+    b.cache[int(b.table[0, where // 64]), where % 64, 5:b.dl:7] = value
+    b.attend()
+    torch.cuda.synchronize()
+    got = b.y.double()
+    clean = where - (length - new)                        # rows of sequence 0 that stand before it
+    before = [r for r in range(new + 1) if r < clean or r == new]
+    clean_cache = b.cache.clone()
+    clean_cache[int(b.table[0, where // 64]), where % 64] = 0
+    y, sigma = attention(clean_cache, b.table, b.cu_host, b.lens_host, b.q, b.q_rope, b.W_uk, b.W_uv, b.scale)
+    tol = 6 * sigma + HALF_STEP[b.out] * (y.abs() + 6 * sigma) + 2.0 ** -16 * y.abs().max()
+    assert ((got - y).abs() <= tol)[before].all()
+    if value != value:
+        assert all(torch.isnan(got[r]).all() for r in range(max(clean, 0), new))
+
+
+@pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("bad", [-1, 10 ** 6, -2 ** 31, 2 ** 31 - 1])
 def test_a_page_outside_the_cache_is_raised(form, bad):
     b = Batch(SMALL, [1, 1], [200, 100], form=form)
