@@ -345,11 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                 int y[4];
 #pragma unroll
                 for (int b = 0; b < 4; ++b) y[b] = __shfl_sync(0xFFFFFFFFu, coord, (t * boxes - base + min(b, boxes - 1)) & 31);
-                {                                                        // the places of the tile's parts, all at once: a lane looks at one
-                    RingAt at = v;
-                    for (int u = 0; u + 1 < lane && u + 1 < NU; ++u) at.next(P::NV);
-                    role_wait_all(lane == 0 ? &r_empty[ro.slot] : (lane <= NU ? &v_empty[at.slot] : nullptr), (lane == 0 ? ro.phase : at.phase) ^ 1, p.status);
-                }
+                role_wait(&r_empty[ro.slot], ro.phase ^ 1, p.status);
                 if (half == 0 && elected()) {
                     mbar_expect_tx(&t_full[f.slot], kRope + NU * kUnit);
 #pragma unroll
@@ -358,6 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                 }
                 ro.next(P::NR);
                 for (int u = 0; u < NU; ++u) {
+                    role_wait(&v_empty[v.slot], v.phase ^ 1, p.status);
                     if (elected()) {
 #pragma unroll
                         for (int b = 0; b < 4; ++b)
@@ -393,7 +390,8 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
             q_phase ^= 1;
             for (int t = w.t0; t < w.t1; ++t, ++n) {
                 const int buf = n & 1;
-                role_wait_all(lane == 0 ? &s_empty[buf] : (lane == 1 ? &t_full[f.slot] : nullptr), lane == 0 ? ((uint32_t)(n >> 1) & 1) ^ 1 : f.phase, p.status);
+                role_wait(&s_empty[buf], ((uint32_t)(n >> 1) & 1) ^ 1, p.status);
+                role_wait(&t_full[f.slot], f.phase, p.status);
                 f.next(kFull);
                 uint32_t at[4];
 #pragma unroll

@@ -280,9 +280,9 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
         }
         const int nt = max(n[0], n[1]);
         const int nkc = (p.dn + 63) / 64, nvc = (p.dv + 63) / 64;        // chunks of keys (and one of rotated parts), of values
-        // (registers: 128 threads of 80 and 256 of 208 are 63488, of the launch's 384 x 168 = 64512)
+        // (registers: 128 threads of 96 and 256 of 200 are 63488, of the launch's 384 x 168 = 64512)
         if (warp >= 4) {
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
             // ========================================= softmax: a thread is a row
             const int i = (warp >> 2) - 1, wq = warp & 3, row = i * 128 + wq * 32 + lane;
             const uint32_t st = tmem + ((uint32_t)(wq * 32) << 16) + i * 128, ot = st + 256;
@@ -338,40 +338,45 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                 float2 sum = make_float2(0.f, 0.f);
                 // P of the first 64 positions goes to the tensor cores while that of the others is made
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
+                for (int c = 0; c < 128; c += 32) {
+                    uint32_t o[16];
 #pragma unroll
-                    for (int c = 0; c < 64; c += 32) {
-                        uint32_t o[16];
-#pragma unroll
-                        for (int j = 0; j < 32; j += 2) {
-                            const float2 e = fma_2(make_float2(__uint_as_float(v[x][c + j]), __uint_as_float(v[x][c + j + 1])), k22, mm2);
-                            float2 w;                                    // (every fourth pair on the multipliers)
-                            if (j % kCubicOf < kCubic) w = exp2_cubic(e);
-                            else w = make_float2(exp2_approx(e.x), exp2_approx(e.y));
-                            if (part) {
-                                if (x * 64 + c + j >= seen) w.x = 0.f;
-                                if (x * 64 + c + j + 1 >= seen) w.y = 0.f;
-                            }
-                            sum = add_2(sum, w);
-                            o[j / 2] = bf16_pair(w.x, w.y);
+                    for (int j = 0; j < 32; j += 2) {
+                        const uint32_t a = v[c / 64][c % 64 + j], b = v[c / 64][c % 64 + j + 1];
+                        const float2 e = fma_2(make_float2(__uint_as_float(a), __uint_as_float(b)), k22, mm2);
+                        float2 w;                                        // (some of the pairs on the multipliers)
+                        if (j % kCubicOf < kCubic) w = exp2_cubic(e);
+                        else w = make_float2(exp2_approx(e.x), exp2_approx(e.y));
+                        if (part) {
+                            if (c + j >= seen) w.x = 0.f;
+                            if (c + j + 1 >= seen) w.y = 0.f;
                         }
-                        tmem_st(st + x * 32 + c / 2, o);                 // (over scores that have been read)
+                        sum = add_2(sum, w);
+                        o[j / 2] = bf16_pair(w.x, w.y);
                     }
-                    tmem_st_wait();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&p_full[2 * i + x]);
+                    if (c == 64) {                                       // (the stores of the first half have had the time of 32 weights)
+                        tmem_st_wait();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&p_full[2 * i]);
+                    }
+                    tmem_st(st + c / 2, o);                              // (over scores that have been read)
                 }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[2 * i + 1]);
                 l += sum.x + sum.y;
             }
             // ---- out
-            const bool have = r0 + row < q.fresh && fits;
             if (mine > 0) {
                 role_wait(&o_done[i], (uint32_t)(mine - 1) & 1, p.status);
                 tc_fence_after();
             }
+            // (by way of this tile's queries, which nothing reads any more: a warp's 32 rows lie apart by all heads, and a row's 16-byte pieces
+            // written one by one took 11000 clocks)
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            const size_t out = ((size_t)(q.a + r0 + row) * p.heads + h) * p.dv;
+            uint8_t* stage = smem + kPQ + i * 3 * kChunk + wq * 8192;
             for (int c = 0; c < p.dv; c += 16) {
                 uint32_t v[16], o[8];
                 if (mine > 0) tmem_ld(ot + c, v);
@@ -386,14 +391,19 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                         o[j] = *reinterpret_cast<const uint32_t*>(&x);
                     } else o[j] = bf16_pair(a, b);
                 }
-                if (have) {
-                    uint4* y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y) + out + c);
-                    y[0] = make_uint4(o[0], o[1], o[2], o[3]);
-                    y[1] = make_uint4(o[4], o[5], o[6], o[7]);
-                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    *reinterpret_cast<uint4*>(stage + lane * 256 + (((c / 8 + x) ^ (lane & 7)) * 16)) = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+            }
+            __syncwarp();
+            const int pieces = p.dv / 8, first = r0 + i * 128 + wq * 32, rows = fits ? min(q.fresh - first, 32) : 0;
+            for (int x = lane; x < rows * pieces; x += 32) {
+                const int rr = x / pieces, c = x - rr * pieces;
+                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y) + ((size_t)(q.a + first + rr) * p.heads + h) * p.dv + c * 8) =
+                    *reinterpret_cast<const uint4*>(stage + rr * 256 + ((c ^ (rr & 7)) * 16));
             }
         } else {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
             if (warp == 0) {
             // ========================================= loads
 #pragma unroll
@@ -448,15 +458,18 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
             auto take = [&](int chunks) { const int a = at; at = (at + chunks) & (kPRing - 1); return a; };
             auto scores = [&](int i, int k) {
                 if (elected()) {
-                    for (int c = 0; c < nkc; ++c) {
-                        const uint32_t a = dq + (((i * 3 + c) * kChunk) >> 4), b = dk + ((((k + c) & (kPRing - 1)) * kChunk) >> 4);
+                    const uint32_t st = tmem + i * 128;
 #pragma unroll
-                        for (int s = 0; s < 4; ++s) umma_ss(tmem + i * 128, a + s * 2, b + s * 2, id_s, c + s > 0);
-                    }
+                    for (int c = 0; c < 2; ++c)
+                        if (c < nkc) {
+                            const uint32_t a = dq + (((i * 3 + c) * kChunk) >> 4), b = dk + ((((k + c) & (kPRing - 1)) * kChunk) >> 4);
+#pragma unroll
+                            for (int s = 0; s < 4; ++s) umma_ss(st, a + s * 2, b + s * 2, id_s, c + s > 0);
+                        }
                     const uint32_t a = dq + (((i * 3 + nkc) * kChunk) >> 4), b = dk + ((((k + nkc) & (kPRing - 1)) * kChunk) >> 4);
 #pragma unroll
                     for (int s = 0; s < 4; ++s)
-                        if (s < rks) umma_ss(tmem + i * 128, a + s * 2, b + s * 2, id_s, true);
+                        if (s < rks) umma_ss(st, a + s * 2, b + s * 2, id_s, true);
                     umma_done(&s_full[i]);
                 }
                 __syncwarp();
@@ -483,48 +496,59 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
             }
             for (int t = 0; t < nt; ++t) {
                 const int v = take(nvc);
-                role_wait(&kv_full[f.slot], f.phase, p.status);
+                const RingAt fv = f;                                     // the values, and the next keys
                 f.next(kPRing);
-                bool next_keys = false;
+                const bool more = t + 1 < nt;
+                const RingAt fk = f;
+                if (more) { k = take(nkc + 1); f.next(kPRing); }
+                const bool whole = nvc == 1 || v + 1 < kPRing;           // (values that go round the ring's end: a chunk at a time)
+                const uint32_t b = dv + ((v * kChunk) >> 4);
+                bool seen_v = false, seen_k = false;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    if (t < n[i]) {
-                        const bool whole = nvc == 1 || v + 1 < kPRing;         // (values that go round the ring's end: a chunk at a time)
-                        const uint32_t b = dv + ((v * kChunk) >> 4), o = tmem + 256 + i * 128, pt = tmem + i * 128;
+                    const uint32_t o = tmem + 256 + i * 128, pt = tmem + i * 128;
+                    auto product = [&](int half) {
+                        if (elected()) {
+                            if (whole) {
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            role_wait(&p_full[2 * i + half], (uint32_t)t & 1, p.status);
-                            tc_fence_after();
-                            if (elected()) {
-                                if (whole) {
+                                for (int s = 0; s < 4; ++s) umma_ts(o, pt + (half * 4 + s) * 8, b + (((half * 4 + s) * 2048) >> 4), id_o, t + half + s > 0);
+                            } else {
+                                const uint32_t id0 = idesc_bf16(128, 64, false, true), id1 = idesc_bf16(128, p.dv - 64, false, true);
 #pragma unroll
-                                    for (int s = half * 4; s < half * 4 + 4; ++s) umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id_o, t > 0 || s > 0);
-                                } else {
-                                    const uint32_t id0 = idesc_bf16(128, 64, false, true), id1 = idesc_bf16(128, p.dv - 64, false, true);
-#pragma unroll
-                                    for (int s = half * 4; s < half * 4 + 4; ++s) {
-                                        umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id0, t > 0 || s > 0);
-                                        umma_ts(o + 64, pt + s * 8, dv + ((s * 2048) >> 4), id1, t > 0 || s > 0);
-                                    }
+                                for (int s = 0; s < 4; ++s) {
+                                    umma_ts(o, pt + (half * 4 + s) * 8, b + (((half * 4 + s) * 2048) >> 4), id0, t + half + s > 0);
+                                    umma_ts(o + 64, pt + (half * 4 + s) * 8, dv + (((half * 4 + s) * 2048) >> 4), id1, t + half + s > 0);
                                 }
-                                if (half == 1) umma_done(&o_done[i]);
                             }
-                            __syncwarp();
+                            if (half == 1) umma_done(&o_done[i]);
                         }
+                        __syncwarp();
+                    };
+                    if (t < n[i]) {
+                        if (!seen_v) role_wait(&kv_full[fv.slot], fv.phase, p.status);
+                        seen_v = true;
+                        role_wait(&p_full[2 * i], (uint32_t)t & 1, p.status);
+                        tc_fence_after();
+                        product(0);
+                        if (t + 1 < n[i] && !seen_k) {
+                            role_wait(&kv_full[fk.slot], fk.phase, p.status);
+                            seen_k = true;
+                        }
+                        role_wait(&p_full[2 * i + 1], (uint32_t)t & 1, p.status);
+                        tc_fence_after();
+                        product(1);
                     }
                     if (i == 1) release();                               // (the values)
                     if (t + 1 < n[i]) {
-                        if (!next_keys) {
-                            k = take(nkc + 1);
-                            role_wait(&kv_full[f.slot], f.phase, p.status);
+                        if (!seen_k) {                                   // (a tile of rows that begins here)
+                            role_wait(&kv_full[fk.slot], fk.phase, p.status);
                             tc_fence_after();
-                            f.next(kPRing);
-                            next_keys = true;
+                            seen_k = true;
                         }
                         scores(i, k);
                     }
                 }
-                if (next_keys) release();
+                if (more) release();
             }
             }
         }
