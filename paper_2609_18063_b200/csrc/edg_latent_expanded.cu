@@ -11,6 +11,8 @@
 // operand of P V from there.  O is rescaled only when a row's maximum has grown by more than 2^8.  Keys and values come by
 // TMA in chunks of 64 columns through one ring of eight (K of a tile, V of it, K of the next: the tile after that takes what S has read).
 // Positions behind a sequence's end are padded to 128; their values are written as zeros, their scores never looked at.
+#include <type_traits>
+
 #include "edg_latent.cuh"
 #include "edg_umma.cuh"
 
@@ -233,29 +235,33 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
 
 // ---------------------------------------------------------------- attention
 
-constexpr int kPThreads = 384;              // warp 0 loads, warp 1 issues products, warps 4-7 and 8-11 a tile of rows each
+constexpr int kPThreads = 640;              // warp 0 loads, warp 1 issues products, warps 4-11 and 12-19 are the softmax of a tile of rows each
 constexpr int kPRing = 8;
 constexpr int kCubicOf = 8, kCubic = 2;     // of 8 weights, 2 are made on the multipliers
-constexpr uint32_t kPQ = 0, kPRingAt = 6 * kChunk, kPBars = kPRingAt + kPRing * kChunk, kPBytes = kPBars + 512 + 1024;
+constexpr uint32_t kPQ = 0, kPRingAt = 6 * kChunk, kPBars = kPRingAt + kPRing * kChunk, kPMax = kPBars + 256, kPBytes = kPMax + 2048;
 
 __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_constant__ ExpandedParams p, const __grid_constant__ CUtensorMap qn_map,
                                                               const __grid_constant__ CUtensorMap qr_map, const __grid_constant__ CUtensorMap k_map,
                                                               const __grid_constant__ CUtensorMap r_map, const __grid_constant__ CUtensorMap v_map) {
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t sb = smem_u32(smem);
     uint64_t* kv_empty = reinterpret_cast<uint64_t*>(smem + kPBars);     // [kPRing] the groups below, read
     uint64_t* kv_full = kv_empty + kPRing;                                  // [kPRing] keys of a tile, its values, the next keys ...: never more than chunks
     uint64_t* q_full = kv_full + kPRing;                                      // [2]
     uint64_t* s_full = q_full + 2;                                       // [2]
-    uint64_t* p_full = s_full + 2;                                       // [2][2] halves of P
-    uint64_t* o_done = p_full + 4;                                       // [2]
+    uint64_t* p_full = s_full + 2;                                       // [2]
+    uint64_t* o_done = p_full + 2;                                       // [2]
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(o_done + 2);
+    float* s_max = reinterpret_cast<float*>(smem + kPMax);               // [tile][half of the columns][row]
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if ((sb & 1023) != 0) {                                              // (the swizzle counts on it)
+        if (tid == 0) latent_raise(p.status, EDG_E_INVAL);
+        return;
+    }
     if (tid == 0) {
         for (int i = 0; i < kPRing; ++i) mbar_init(&kv_empty[i], 1);
         for (int i = 0; i < kPRing; ++i) mbar_init(&kv_full[i], 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&q_full[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[2 * i], 4); mbar_init(&p_full[2 * i + 1], 4); mbar_init(&o_done[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&q_full[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 8); mbar_init(&o_done[i], 1); }
         fence_barrier_init();
     }
     if (warp == 1) tmem_alloc(s_tmem, 512);
@@ -280,51 +286,54 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
         }
         const int nt = max(n[0], n[1]);
         const int nkc = (p.dn + 63) / 64, nvc = (p.dv + 63) / 64;        // chunks of keys (and one of rotated parts), of values
-        // (registers: 128 threads of 96 and 256 of 200 are 63488, of the launch's 384 x 168 = 64512)
         if (warp >= 4) {
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
-            // ========================================= softmax: a thread is a row
-            const int i = (warp >> 2) - 1, wq = warp & 3, row = i * 128 + wq * 32 + lane;
+            // ========================================= softmax: two threads to a row, 64 columns each (one thread's 128 took 2000 clocks from S to P,
+            // on the way from one product of a tile to the next)
+            const int i = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, wq = warp & 3, row = i * 128 + wq * 32 + lane;
             const uint32_t st = tmem + ((uint32_t)(wq * 32) << 16) + i * 128, ot = st + 256;
             const float k2 = p.scale * 1.4426950408889634f;
             const int pos = pos0 + row;                                  // positions 0 .. pos are seen
-            float m = -INFINITY, l = 0.f;
+            float* my_max = s_max + (i * 2 + half) * 128 + wq * 32 + lane;
+            const float* their_max = s_max + (i * 2 + 1 - half) * 128 + wq * 32 + lane;
+            float m = -INFINITY, l = 0.f;                                // (l: of this thread's columns)
             const int mine = i == 0 ? n[0] : n[1];
             for (int t = 0; t < mine; ++t) {
                 role_wait(&s_full[i], (uint32_t)t & 1, p.status);
                 tc_fence_after();
-                const int seen = pos + 1 - t * 128;                      // of this tile
-                const bool part = __any_sync(0xFFFFFFFFu, seen < 128);
-                // 128 scores of the row in registers, the largest of them
-                uint32_t v[2][64];
+                const int seen = pos + 1 - t * 128 - half * 64;          // of these columns
+                const bool part = __any_sync(0xFFFFFFFFu, seen < 64);
+                uint32_t v[64];
+                tmem_ld(st + half * 64, v);
                 float mt;
                 {
                     float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    if (part) {
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        tmem_ld(st + x * 64, v[x]);
-                        if (part) {
-#pragma unroll
-                            for (int j = 0; j < 64; ++j)
-                                if (x * 64 + j >= seen) v[x][j] = 0xFF800000u;
-                        }
-#pragma unroll
-                        for (int j = 0; j < 64; j += 8)
-#pragma unroll
-                            for (int y = 0; y < 4; ++y) a[y] = max3(a[y], __uint_as_float(v[x][j + y]), __uint_as_float(v[x][j + 4 + y]));
+                        for (int j = 0; j < 64; ++j)
+                            if (j >= seen) v[j] = 0xFF800000u;
                     }
-                    mt = max3(max3(a[0], a[1], a[2]), a[3], a[3]) * k2;  // (the scale is positive)
+#pragma unroll
+                    for (int j = 0; j < 64; j += 8)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) a[y] = max3(a[y], __uint_as_float(v[j + y]), __uint_as_float(v[j + 4 + y]));
+                    mt = max3(max3(a[0], a[1], a[2]), a[3], a[3]);
+                    // the other half's (whose reader is done with it before the next S can be there: it takes all of P)
+                    *my_max = mt;
+                    tc_fence_before();
+                    barrier_sync(1 + i, 256);
+                    tc_fence_after();
+                    mt = max3(mt, *their_max, *their_max) * k2;          // (the scale is positive)
                     if (!(mt < INFINITY)) { l = __int_as_float(0x7FFFFFFF); mt = -INFINITY; }      // NaN or infinity among them: so is the row
                     mt = fmaxf(m, mt);
                 }
                 if (t == 0) m = mt;
                 const bool grown = mt > m + 8.f;
-                if (__any_sync(0xFFFFFFFFu, grown)) {
+                if (__any_sync(0xFFFFFFFFu, grown)) {                    // (the same rows in both halves; each takes every second 16 columns of O)
                     const float alpha = grown ? exp2_approx(m - mt) : 1.f;
                     if (grown) { m = mt; l *= alpha; }
                     role_wait(&o_done[i], (uint32_t)(t - 1) & 1, p.status);
                     tc_fence_after();
-                    for (int c = 0; c < p.dv; c += 16) {
+                    for (int c = half * 16; c < p.dv; c += 32) {
                         uint32_t o[16];
                         tmem_ld(ot + c, o);
 #pragma unroll
@@ -334,38 +343,30 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                     tmem_st_wait();
                 }
                 const float mm = m == -INFINITY ? 0.f : -m;
-                const float2 k22 = make_float2(k2, k2), mm2 = make_float2(mm, mm);
                 float2 sum = make_float2(0.f, 0.f);
-                // P of the first 64 positions goes to the tensor cores while that of the others is made
+                // (masked scores are -infinity: ex2 makes zeros of them, the cubic would not)
+                auto weights = [&](auto cubic) {
 #pragma unroll
-                for (int c = 0; c < 128; c += 32) {
-                    uint32_t o[16];
+                    for (int c = 0; c < 64; c += 32) {
+                        uint32_t o[16];
 #pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        const uint32_t a = v[c / 64][c % 64 + j], b = v[c / 64][c % 64 + j + 1];
-                        const float2 e = fma_2(make_float2(__uint_as_float(a), __uint_as_float(b)), k22, mm2);
-                        float2 w;                                        // (some of the pairs on the multipliers)
-                        if (j % kCubicOf < kCubic) w = exp2_cubic(e);
-                        else w = make_float2(exp2_approx(e.x), exp2_approx(e.y));
-                        if (part) {
-                            if (c + j >= seen) w.x = 0.f;
-                            if (c + j + 1 >= seen) w.y = 0.f;
+                        for (int j = 0; j < 32; j += 2) {
+                            const float a = fmaf(__uint_as_float(v[c + j]), k2, mm), b = fmaf(__uint_as_float(v[c + j + 1]), k2, mm);
+                            const bool multiply = decltype(cubic)::value && j % kCubicOf < kCubic;
+                            const float x = multiply ? exp2_cubic(a) : exp2_approx(a), y = multiply ? exp2_cubic(b) : exp2_approx(b);
+                            sum.x += x;
+                            sum.y += y;
+                            o[j / 2] = bf16_pair(x, y);
                         }
-                        sum = add_2(sum, w);
-                        o[j / 2] = bf16_pair(w.x, w.y);
+                        tmem_st(st + half * 32 + c / 2, o);              // (over the scores of the first half, which all have read: the barrier above)
                     }
-                    if (c == 64) {                                       // (the stores of the first half have had the time of 32 weights)
-                        tmem_st_wait();
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&p_full[2 * i]);
-                    }
-                    tmem_st(st + c / 2, o);                              // (over scores that have been read)
-                }
+                };
+                if (part) weights(std::false_type());
+                else weights(std::true_type());
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[2 * i + 1]);
+                if (lane == 0) mbar_arrive(&p_full[i]);
                 l += sum.x + sum.y;
             }
             // ---- out
@@ -373,11 +374,13 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                 role_wait(&o_done[i], (uint32_t)(mine - 1) & 1, p.status);
                 tc_fence_after();
             }
-            // (by way of this tile's queries, which nothing reads any more: a warp's 32 rows lie apart by all heads, and a row's 16-byte pieces
-            // written one by one took 11000 clocks)
+            *my_max = l;
+            barrier_sync(1 + i, 256);
+            l += *their_max;
+            // (by way of this tile's queries, which nothing reads any more; the two halves take every second 16 columns, then every second row)
             const float inv = l == 0.f ? 0.f : 1.f / l;
             uint8_t* stage = smem + kPQ + i * 3 * kChunk + wq * 8192;
-            for (int c = 0; c < p.dv; c += 16) {
+            for (int c = half * 16; c < p.dv; c += 32) {
                 uint32_t v[16], o[8];
                 if (mine > 0) tmem_ld(ot + c, v);
                 else
@@ -395,15 +398,14 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                 for (int x = 0; x < 2; ++x)
                     *reinterpret_cast<uint4*>(stage + lane * 256 + (((c / 8 + x) ^ (lane & 7)) * 16)) = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
             }
-            __syncwarp();
+            barrier_sync(1 + i, 256);
             const int pieces = p.dv / 8, first = r0 + i * 128 + wq * 32, rows = fits ? min(q.fresh - first, 32) : 0;
-            for (int x = lane; x < rows * pieces; x += 32) {
+            for (int x = half * 32 + lane; x < rows * pieces; x += 64) {
                 const int rr = x / pieces, c = x - rr * pieces;
                 *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y) + ((size_t)(q.a + first + rr) * p.heads + h) * p.dv + c * 8) =
                     *reinterpret_cast<const uint4*>(stage + rr * 256 + ((c ^ (rr & 7)) * 16));
             }
         } else {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
             if (warp == 0) {
             // ========================================= loads
 #pragma unroll
@@ -507,36 +509,30 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const uint32_t o = tmem + 256 + i * 128, pt = tmem + i * 128;
-                    auto product = [&](int half) {
-                        if (elected()) {
-                            if (whole) {
-#pragma unroll
-                                for (int s = 0; s < 4; ++s) umma_ts(o, pt + (half * 4 + s) * 8, b + (((half * 4 + s) * 2048) >> 4), id_o, t + half + s > 0);
-                            } else {
-                                const uint32_t id0 = idesc_bf16(128, 64, false, true), id1 = idesc_bf16(128, p.dv - 64, false, true);
-#pragma unroll
-                                for (int s = 0; s < 4; ++s) {
-                                    umma_ts(o, pt + (half * 4 + s) * 8, b + (((half * 4 + s) * 2048) >> 4), id0, t + half + s > 0);
-                                    umma_ts(o + 64, pt + (half * 4 + s) * 8, dv + (((half * 4 + s) * 2048) >> 4), id1, t + half + s > 0);
-                                }
-                            }
-                            if (half == 1) umma_done(&o_done[i]);
-                        }
-                        __syncwarp();
-                    };
                     if (t < n[i]) {
                         if (!seen_v) role_wait(&kv_full[fv.slot], fv.phase, p.status);
                         seen_v = true;
-                        role_wait(&p_full[2 * i], (uint32_t)t & 1, p.status);
-                        tc_fence_after();
-                        product(0);
                         if (t + 1 < n[i] && !seen_k) {
                             role_wait(&kv_full[fk.slot], fk.phase, p.status);
                             seen_k = true;
                         }
-                        role_wait(&p_full[2 * i + 1], (uint32_t)t & 1, p.status);
+                        role_wait(&p_full[i], (uint32_t)t & 1, p.status);
                         tc_fence_after();
-                        product(1);
+                        if (elected()) {
+                            if (whole) {
+#pragma unroll
+                                for (int s = 0; s < 8; ++s) umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id_o, t + s > 0);
+                            } else {
+                                const uint32_t id0 = idesc_bf16(128, 64, false, true), id1 = idesc_bf16(128, p.dv - 64, false, true);
+#pragma unroll
+                                for (int s = 0; s < 8; ++s) {
+                                    umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id0, t + s > 0);
+                                    umma_ts(o + 64, pt + s * 8, dv + ((s * 2048) >> 4), id1, t + s > 0);
+                                }
+                            }
+                            umma_done(&o_done[i]);
+                        }
+                        __syncwarp();
                     }
                     if (i == 1) release();                               // (the values)
                     if (t + 1 < n[i]) {

@@ -127,36 +127,22 @@ __device__ __forceinline__ float exp2_approx(float v) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-// the largest of three, NaN if one of them is; two values of a * b + c, and of a + b, in one instruction
+// the largest of three, NaN if one of them is
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-__device__ __forceinline__ float2 fma_2(float2 a, float2 b, float2 c) {
-    float2 r;
-    asm("{\n.reg .b64 a, b, c;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 a, a, b, c;\nmov.b64 {%0, %1}, a;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return r;
-}
-__device__ __forceinline__ float2 add_2(float2 a, float2 b) {
-    float2 r;
-    asm("{\n.reg .b64 a, b;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
-// 2^x of two values on the multipliers, for what the unit of ex2 has no time for: x is split into an integer and a rest in [-1/2, 1/2] (Cody and
-// Waite's reduction, by the rounding of an addition), 2^rest is a cubic (minimax of the relative error, 7.5e-5, by Remez exchange), the integer
-// goes into the exponent.  x <= 127; below -126 it counts as -126.
-__device__ __forceinline__ float2 exp2_cubic(float2 x) {
-    x.x = fmaxf(x.x, -126.f);
-    x.y = fmaxf(x.y, -126.f);
-    const float2 big = make_float2(12582912.f, 12582912.f), t = add_2(x, big);
-    const float2 f = add_2(x, make_float2(12582912.f - t.x, 12582912.f - t.y));
-    float2 p = fma_2(make_float2(0.0551716685f, 0.0551716685f), f, make_float2(0.2426111251f, 0.2426111251f));
-    p = fma_2(p, f, make_float2(0.6932609677f, 0.6932609677f));
-    p = fma_2(p, f, make_float2(0.9999280572f, 0.9999280572f));
-    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+// 2^x on the multipliers, for what the unit of ex2 has no time for: x is split into an integer and a rest in [-1/2, 1/2] (Cody and Waite's
+// reduction, by the rounding of an addition), 2^rest is a cubic (minimax of the relative error, 7.5e-5, by Remez exchange), the integer goes into
+// the exponent.  x <= 127; below -126 it counts as -126.  (17 values a clock and SM beside ex2's 16; the compiler pairs the additions and products.)
+__device__ __forceinline__ float exp2_cubic(float x) {
+    x = fmaxf(x, -126.f);
+    const float t = x + 12582912.f, f = x - (t - 12582912.f);
+    float p = fmaf(0.0551716685f, f, 0.2426111251f);
+    p = fmaf(p, f, 0.6932609677f);
+    p = fmaf(p, f, 0.9999280572f);
+    return __uint_as_float(__float_as_uint(p) + (__float_as_uint(t) << 23));
 }
 // the largest magnitudes so far of the bf16 values of 16 bytes, as bits; whether one of them is infinite or NaN
 __device__ __forceinline__ uint32_t bf16_magnitudes(uint32_t m, uint4 v) {
