@@ -81,6 +81,7 @@ struct LinearParams {
     int cluster, cta_blocks;    // CTAs that share the input dimension; blocks of each
     float lora_scale;
 };
+static_assert(kThreads % (kWarps * 16) == 0, "a thread keeps its row");
 
 // u[t][r] = A[r] . x[t]: a warp per (token, rank)
 __global__ void __launch_bounds__(128) linear_u_kernel(const uint16_t* A, const uint16_t* x, float* u, int Kd, int ldx, int rank) {
@@ -103,9 +104,9 @@ __global__ void __launch_bounds__(128) linear_u_kernel(const uint16_t* A, const 
 }
 
 // Shared memory: activations [blocks][4 chunks][NT][32 lanes] 16 bytes; sums of them [blocks][128/GS][NT * 8] float; scales of the tokens
-// [NT * 8]; partial sums [kWarps][16 rows][NT * 8] float.
-template <int GS, int NT> constexpr size_t linear_smem(int blocks) {
-    return (size_t)blocks * (NT * 2048 + (128 / GS) * NT * 32) + NT * 8 * 4 + kWarps * 16 * NT * 8 * 4;
+// [NT * 8]; partial sums [kWarps][16 rows][NT * 8] float; A x of the tokens [NT * 8][rank rounded to 8] float.
+template <int GS, int NT> constexpr size_t linear_smem(int blocks, int rank) {
+    return (size_t)blocks * (NT * 2048 + (128 / GS) * NT * 32) + NT * 8 * 4 + kWarps * 16 * NT * 8 * 4 + (size_t)NT * 32 * ((rank + 7) & ~7);
 }
 
 // CTAs that share an SM, by the registers of NT tiles of tokens
@@ -120,6 +121,8 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
     float* s_sum = reinterpret_cast<float*>(smem + (size_t)p.cta_blocks * NT * 2048);
     float* s_scale = s_sum + (size_t)p.cta_blocks * PB * TN;
     float* s_red = s_scale + TN;
+    float* s_u = s_red + kWarps * 16 * TN;
+    const int ru = (p.rank + 7) & ~7;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
     const int rank_c = (int)(blockIdx.x % p.cluster), unit0 = (int)(blockIdx.x / p.cluster), n_units_grid = (int)(gridDim.x / p.cluster);
     const int t0 = blockIdx.y * TN, nt = min(TN, p.T - t0);
@@ -173,17 +176,36 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
             if (n < nt && k < p.Kd) return __ldg(reinterpret_cast<const uint4*>(p.x + (size_t)(t0 + n) * p.ldx + k));
             return make_uint4(0, 0, 0, 0);
         };
+        // Groups of GS codes go to the warps in turn.  The first ones stay in registers from the search for the largest magnitude to the
+        // operands; what does not fit is read again.
+        constexpr int GC = GS / 32, kRoom = NT <= 2 ? 8 : 16, kKeep = kRoom / (NT * GC) > 0 ? kRoom / (NT * GC) : 1;
+        uint4 keep[kKeep][GC][NT];
         uint32_t m[NT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) m[j] = 0u;
-#pragma unroll 2
-        for (int c = warp; c < chunks; c += kWarps)
+        auto magnitude = [&](int j, const uint4& v) {
+            const float f[8] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y), bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)};
+            m[j] = max(m[j], abs_max8(f));
+        };
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const uint4 v = raw(c, j * 8 + g);
-                const float f[8] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y), bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)};
-                m[j] = max(m[j], abs_max8(f));
-            }
+        for (int i = 0; i < kKeep; ++i) {
+            const int c = (warp + i * kWarps) * GC;
+#pragma unroll
+            for (int x = 0; x < GC; ++x)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) keep[i][x][j] = c < chunks ? raw(c + x, j * 8 + g) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i)
+#pragma unroll
+            for (int x = 0; x < GC; ++x)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) magnitude(j, keep[i][x][j]);
+        for (int c = (warp + kKeep * kWarps) * GC; c < chunks; c += kWarps * GC)
+#pragma unroll
+            for (int x = 0; x < GC; ++x)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) magnitude(j, raw(c + x, j * 8 + g));
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             const uint32_t v = group_max<4>(m[j]);
@@ -193,19 +215,37 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
         float sc[NT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) sc[j] = vector_scale(s_max[j * 8 + g]);
-        for (int c = warp * (GS / 32); c < chunks; c += kWarps * (GS / 32))
+        auto operands = [&](int c, int j, const uint4 (&v)[GC]) {
+            float sum = 0.f;
+#pragma unroll
+            for (int x = 0; x < GC; ++x) {
+                const float f[8] = {bf16_lo(v[x].x), bf16_hi(v[x].x), bf16_lo(v[x].y), bf16_hi(v[x].y), bf16_lo(v[x].z), bf16_hi(v[x].z), bf16_lo(v[x].w), bf16_hi(v[x].w)};
+                s_x[(size_t)((c + x) * NT + j) * 32 + lane] = permute8_s(f, sc[j]);
+                sum += ((f[0] + f[1]) + (f[2] + f[3])) * sc[j] + ((f[4] + f[5]) + (f[6] + f[7])) * sc[j];
+            }
+            sum = group_sum<4>(sum);
+            if (t4 == 0) s_sum[(c / GC) * TN + j * 8 + g] = sum * kScaleS;
+        };
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i) {
+            const int c = (warp + i * kWarps) * GC;
+            if (c < chunks) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    uint4 v[GC];
+#pragma unroll
+                    for (int x = 0; x < GC; ++x) v[x] = keep[i][x][j];
+                    operands(c, j, v);
+                }
+            }
+        }
+        for (int c = (warp + kKeep * kWarps) * GC; c < chunks; c += kWarps * GC)
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                float sum = 0.f;
+                uint4 v[GC];
 #pragma unroll
-                for (int i = 0; i < GS / 32; ++i) {
-                    const uint4 v = raw(c + i, j * 8 + g);
-                    const float f[8] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y), bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)};
-                    s_x[(size_t)((c + i) * NT + j) * 32 + lane] = permute8_s(f, sc[j]);
-                    sum += ((f[0] + f[1]) + (f[2] + f[3])) * sc[j] + ((f[4] + f[5]) + (f[6] + f[7])) * sc[j];
-                }
-                sum = group_sum<4>(sum);
-                if (t4 == 0) s_sum[(c / (GS / 32)) * TN + j * 8 + g] = sum * kScaleS;
+                for (int x = 0; x < GC; ++x) v[x] = raw(c + x, j * 8 + g);
+                operands(c, j, v);
             }
         __syncthreads();
         if (tid < TN) s_scale[tid] = kUnscaleS * vector_unscale(vector_scale(s_max[tid]));
@@ -269,42 +309,90 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
             *reinterpret_cast<float2*>(red + g * TN + j * 8 + 2 * t4) = make_float2(acc[j][0], acc[j][1]);
             *reinterpret_cast<float2*>(red + (g + 8) * TN + j * 8 + 2 * t4) = make_float2(acc[j][2], acc[j][3]);
         }
-        if (p.cluster > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
-        if (!u_there) { pdl_wait_prior_grid(); u_there = true; }
-        // outputs of the unit, spread over the cluster's CTAs; consecutive threads take consecutive rows of a token
-        const int outs = wr * 16 * nt;
-        for (int o = rank_c * kThreads + tid; o < outs; o += p.cluster * kThreads) {
-            const int row = o % (wr * 16), tok = o / (wr * 16), rt = row >> 4;
-            const int n = (unit * wr + rt) * 16 + (row & 15);
-            if (n >= p.N) continue;
+        __syncthreads();
+        if (p.cluster > 1) {                           // this CTA's sums over its warps, scaled, into the first warp's of each row tile
+            for (int o = tid; o < wr * 16 * TN; o += kThreads) {
+                const int x = o / (16 * TN), at = o - x * 16 * TN;
+                float* s = s_red + x * p.wk * 16 * TN + at;
+                float v = s[0];
+                for (int k = 1; k < p.wk; ++k) v += s[k * 16 * TN];
+                s[0] = v * s_scale[at % TN];
+            }
+            __syncwarp();
+            cluster_arrive();
+            cluster_wait();
+        }
+        if (!u_there) {                                // (A x comes from the kernel before, which has run beside this one)
+            pdl_wait_prior_grid();
+            for (int i = tid; i < nt * ru; i += kThreads) {
+                const int tok = i / ru, r = i - tok * ru;
+                s_u[i] = r < p.rank ? p.lora_scale * __ldcg(p.u + (size_t)(t0 + tok) * p.rank + r) : 0.f;
+            }
+            __syncthreads();
+            u_there = true;
+        }
+        // outputs of the unit, spread over the cluster's CTAs: a thread keeps its row, consecutive threads take consecutive rows
+        const int rows = wr * 16, row = tid & (rows - 1), rt = row >> 4, n = (unit * wr + rt) * 16 + (row & 15);
+        const int tstep = p.cluster * kThreads / rows, tok0 = (rank_c * kThreads + tid) / rows;
+        const float* src = s_red + rt * p.wk * 16 * TN + (row & 15) * TN;
+        auto value = [&](int tok) {
             float v = 0.f;
-            const float* src = s_red + rt * p.wk * 16 * TN + (row & 15) * TN + tok;
             if (p.cluster > 1) {
-                for (int c = 0; c < p.cluster; ++c) {
-                    float part = 0.f, us;
-                    for (int k = 0; k < p.wk; ++k) {
-                        float f;
-                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(map_to_cta(src + k * 16 * TN, c)));
-                        part += f;
-                    }
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(us) : "r"(map_to_cta(s_scale + tok, c)));
-                    v = fmaf(part, us, v);
-                }
+                float f[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (c < p.cluster) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f[c]) : "r"(map_to_cta(src + tok, c)));
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (c < p.cluster) v += f[c];
             } else {
-                for (int k = 0; k < p.wk; ++k) v += src[k * 16 * TN];
+                for (int k = 0; k < p.wk; ++k) v += src[tok + k * 16 * TN];
                 v *= s_scale[tok];
             }
-            if (p.rank > 0) {
-                const uint16_t* Bn = p.B + (size_t)n * p.rank;
-                const float* ut = p.u + (size_t)(t0 + tok) * p.rank;
-                float e = 0.f;
-                for (int r = 0; r < p.rank; ++r) e = fmaf(bf16_bits_to_float(Bn[r]), __ldcg(ut + r), e);
-                v = fmaf(p.lora_scale, e, v);
-            }
+            return v;
+        };
+        auto store = [&](int tok, float v) {
             const size_t at = (size_t)(t0 + tok) * p.ldy + n;
             if (p.out_dtype == EDG_F32) store_out(static_cast<float*>(p.y), at, v);
             else if (p.out_dtype == EDG_F16) store_out(static_cast<__half*>(p.y), at, v);
             else static_cast<uint16_t*>(p.y)[at] = bf16_rn(v);
+        };
+        if (n < p.N) {
+            if (p.rank == 0) {
+                for (int tok = tok0; tok < nt; tok += tstep) store(tok, value(tok));
+            } else {
+                // four tokens at a time against eight ranks of this row of B
+                const uint16_t* Bn = p.B + (size_t)n * p.rank;
+                const bool wide = (p.rank & 7) == 0;
+                for (int q0 = tok0; q0 < nt; q0 += 4 * tstep) {
+                    float e[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) e[q] = q0 + q * tstep < nt ? value(q0 + q * tstep) : 0.f;
+                    for (int r = 0; r < ru; r += 8) {
+                        float bv[8];
+                        if (wide) {
+                            const uint4 w = __ldg(reinterpret_cast<const uint4*>(Bn + r));
+                            bv[0] = bf16_lo(w.x); bv[1] = bf16_hi(w.x); bv[2] = bf16_lo(w.y); bv[3] = bf16_hi(w.y);
+                            bv[4] = bf16_lo(w.z); bv[5] = bf16_hi(w.z); bv[6] = bf16_lo(w.w); bv[7] = bf16_hi(w.w);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) bv[j] = r + j < p.rank ? bf16_bits_to_float(Bn[r + j]) : 0.f;
+                        }
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int tok = q0 + q * tstep;
+                            if (tok < nt) {
+                                const float4 a = *reinterpret_cast<const float4*>(s_u + tok * ru + r), b = *reinterpret_cast<const float4*>(s_u + tok * ru + r + 4);
+                                e[q] = fmaf(bv[0], a.x, e[q]); e[q] = fmaf(bv[1], a.y, e[q]); e[q] = fmaf(bv[2], a.z, e[q]); e[q] = fmaf(bv[3], a.w, e[q]);
+                                e[q] = fmaf(bv[4], b.x, e[q]); e[q] = fmaf(bv[5], b.y, e[q]); e[q] = fmaf(bv[6], b.z, e[q]); e[q] = fmaf(bv[7], b.w, e[q]);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (q0 + q * tstep < nt) store(q0 + q * tstep, e[q]);
+                }
+            }
         }
         __syncwarp();
         // (the next unit's partial sums wait until these have been read)
@@ -313,44 +401,58 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
     if (!u_there) pdl_wait_prior_grid();
 }
 
-template <int GS, int NT> int32_t launch_linear(LinearParams& p, cudaStream_t st) {
-    static OncePerDevice once;
-    constexpr size_t kMost = 200 * 1024;
-    EDG_CUDA_TRY(once([] { return allow_smem(kMost, linear_kernel<GS, NT>); }));
-    const int sms = sm_count();
-    // row tiles that a CTA takes at a time: one, all warps on it, unless there are many more than SMs
-    p.wk = kWarps;
-    while (p.wk > 2 && p.tiles / (kWarps / p.wk) > 16 * sms) p.wk >>= 1;
-    const int units = (p.tiles + kWarps / p.wk - 1) / (kWarps / p.wk);
+constexpr size_t kMost = 200 * 1024;
+struct LinearPlan { int nt, wk, cluster, cta_blocks, grid; size_t smem; int64_t cost; };
+
+// Tokens of a pass (8 NT), warps that share a row tile, CTAs that share the input dimension: what takes the least by the rounds that a CTA's
+// warps make.  In clocks: a block of 128 codes 150 + 110 NT of a warp with seven beside it, the sums' meeting 700 + 60 NT and 1500 more in a
+// cluster, the activations 1500 + 60 NT a block at the start.
+template <int GS, int NT> void plan_linear(const LinearParams& p, int sms, LinearPlan& best) {
     const int slices = (p.T + NT * 8 - 1) / (NT * 8);
-    // CTAs of a cluster share the input dimension: as many as shared memory asks for, and more while there are SMs without work
-    // and each keeps a block for every warp
-    p.cluster = 1;
-    auto bytes = [&](int c) { return linear_smem<GS, NT>((p.blocks + c - 1) / c); };
-    while (p.cluster < 8 && (bytes(p.cluster) > kMost || ((int64_t)units * slices * p.cluster * 2 <= sms && p.blocks >= 2 * p.cluster * kWarps)))
-        p.cluster *= 2;
-    if (bytes(p.cluster) > kMost) return EDG_E_SHAPE;
-    p.cta_blocks = (p.blocks + p.cluster - 1) / p.cluster;
-    const size_t smem = bytes(p.cluster);
-    int resident = (int)((220 * 1024) / (smem + 1024));
-    resident = resident < 1 ? 1 : (resident > kResident<NT> ? kResident<NT> : resident);
-    const int most = (sms * resident / p.cluster > 0 ? sms * resident / p.cluster : 1);
-    const int waves = (units + most - 1) / most;
-    const int grid = (units + waves - 1) / waves;
-    EDG_CUDA_TRY(p.rank > 0 ? launch_pdl_cluster(p.cluster, linear_kernel<GS, NT>, dim3(grid * p.cluster, slices), kThreads, smem, st, p)
-                            : launch_cluster(p.cluster, linear_kernel<GS, NT>, dim3(grid * p.cluster, slices), kThreads, smem, st, p));
+    for (int c = 1; c <= 8; c *= 2)
+        for (int wk = 1; wk <= kWarps; wk *= 2) {
+            const int each = (p.blocks + c - 1) / c;
+            const size_t bytes = linear_smem<GS, NT>(each, p.rank);
+            if (bytes > kMost || (c > 1 && each * (c - 1) >= p.blocks)) continue;      // (every CTA has blocks)
+            int resident = (int)((220 * 1024) / (bytes + 1024));
+            resident = resident < 1 ? 1 : (resident > kResident<NT> ? kResident<NT> : resident);
+            const int units = (p.tiles + kWarps / wk - 1) / (kWarps / wk), room = sms * resident / c > 0 ? sms * resident / c : 1;
+            const int64_t all = (int64_t)units * slices, rounds = (all + room - 1) / room;
+            const int beside = all * c > sms ? resident : 1;                           // CTAs that share an SM's pipes
+            const int64_t cost = rounds * ((int64_t)((each + wk - 1) / wk) * (150 + 110 * NT) * beside + 700 + 60 * NT + (c > 1 ? 1500 : 0)) +
+                                 (int64_t)(1500 + each * 60 * NT) * (slices > 1 ? (slices * c + sms - 1) / sms : 1);
+            if (best.cost >= 0 && cost >= best.cost) continue;
+            const int waves = (units + room - 1) / room;
+            best = {NT, wk, c, each, (units + waves - 1) / waves, bytes, cost};
+        }
+}
+
+template <int GS, int NT> int32_t launch_linear(LinearParams& p, const LinearPlan& plan, cudaStream_t st) {
+    static OncePerDevice once;
+    EDG_CUDA_TRY(once([] { return allow_smem(kMost, linear_kernel<GS, NT>); }));
+    p.wk = plan.wk;
+    p.cluster = plan.cluster;
+    p.cta_blocks = plan.cta_blocks;
+    const dim3 grid(plan.grid * plan.cluster, (p.T + NT * 8 - 1) / (NT * 8));
+    EDG_CUDA_TRY(p.rank > 0 ? launch_pdl_cluster(p.cluster, linear_kernel<GS, NT>, grid, kThreads, plan.smem, st, p)
+                            : launch_cluster(p.cluster, linear_kernel<GS, NT>, grid, kThreads, plan.smem, st, p));
     return EDG_OK;
 }
 
 template <int GS> int32_t launch_gs(LinearParams& p, cudaStream_t st) {
-    // as many tokens a pass as there are, up to 64, and fewer where their activations do not fit the shared memory of eight CTAs
-    int nt = p.T <= 8 ? 1 : (p.T <= 16 ? 2 : (p.T <= 32 ? 4 : 8));
-    while (nt > 1 && (size_t)((p.blocks + 7) / 8) * nt * (2048 + 32 * (128 / GS)) + nt * 8 * 4 * 129 > 200 * 1024) nt >>= 1;
-    switch (nt) {
-        case 1: return launch_linear<GS, 1>(p, st);
-        case 2: return launch_linear<GS, 2>(p, st);
-        case 4: return launch_linear<GS, 4>(p, st);
-        default: return launch_linear<GS, 8>(p, st);
+    const int sms = sm_count();
+    LinearPlan plan;
+    plan.cost = -1;
+    plan_linear<GS, 1>(p, sms, plan);
+    if (p.T > 8) plan_linear<GS, 2>(p, sms, plan);
+    if (p.T > 16) plan_linear<GS, 4>(p, sms, plan);
+    if (p.T > 32) plan_linear<GS, 8>(p, sms, plan);
+    if (plan.cost < 0) return EDG_E_SHAPE;
+    switch (plan.nt) {
+        case 1: return launch_linear<GS, 1>(p, plan, st);
+        case 2: return launch_linear<GS, 2>(p, plan, st);
+        case 4: return launch_linear<GS, 4>(p, plan, st);
+        default: return launch_linear<GS, 8>(p, plan, st);
     }
 }
 
