@@ -135,14 +135,9 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
     // ---- the first blocks of codes are asked for before anything else
     uint4 c0[kAhead], c1[kAhead];
     uint32_t z0[kAhead][PB], z1[kAhead][PB];
-    auto load = [&](int slot, int unit, int i) {
-        const int tile = unit * wr + my_tile;
-        if (tile >= p.tiles) return;
-        const size_t blk = (size_t)tile * p.blocks + b0 + my_k + i * p.wk;
-        const uint8_t* c = p.codes + blk * 1024 + lane * 16;
+    auto load = [&](int slot, const uint8_t* c, const uint8_t* z) {
         c0[slot] = ld_stream16(c);
         c1[slot] = ld_stream16(c + 512);
-        const uint8_t* z = p.sz + blk * (64 * PB) + g * (4 * PB);
         if constexpr (PB == 1) {
             z0[slot][0] = ld_stream4(z);
             z1[slot][0] = ld_stream4(z + 32);
@@ -155,15 +150,26 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
             z1[slot][0] = b.x; z1[slot][1] = b.y; z1[slot][2] = b.z; z1[slot][3] = b.w;
         }
     };
-    int lu = unit0, li = 0;                            // the next block to ask for
+    // A warp's blocks of a unit, rounded up to the slots: a block's slot is its number, known when the loop is unrolled.
+    const int padded = (per_unit + kAhead - 1) / kAhead * kAhead;
+    int lu = unit0, li = 0;                            // the next block to ask for, and where it lies
+    const size_t first = ((size_t)(unit0 * wr + my_tile) * p.blocks + b0 + my_k), jump = (size_t)n_units_grid * wr * p.blocks - (size_t)padded * p.wk;
+    const uint8_t *lc = p.codes + first * 1024 + lane * 16, *lz = p.sz + first * (64 * PB) + g * (4 * PB);
     auto load_next = [&](int slot) {
-        if (lu < units && per_unit > 0) {
-            load(slot, lu, li);
-            if (++li == per_unit) { li = 0; lu += n_units_grid; }
+        if (li < per_unit && lu * wr + my_tile < p.tiles) load(slot, lc, lz);
+        lc += p.wk * 1024;
+        lz += p.wk * 64 * PB;
+        if (++li == padded) {
+            li = 0;
+            lu += n_units_grid;
+            lc += jump * 1024;
+            lz += jump * (64 * PB);
         }
     };
+    if (padded > 0) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) load_next(j);
+        for (int j = 0; j < kAhead; ++j) load_next(j);
+    }
 
     // ---- activations: largest magnitude per token, then operands and sums of groups
     {
@@ -253,13 +259,11 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
     }
 
     bool u_there = p.rank == 0;
-    int slot = 0;
     for (int unit = unit0; unit < units; unit += n_units_grid) {
         const int tile = unit * wr + my_tile;
         float acc[NT][4];
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
-        // (the slots are walked by a switch over kAhead constants: registers cannot be indexed)
         auto block = [&](int s, int i) {
             const int lb = my_k + i * p.wk;            // block within this CTA's
             const uint32_t w0[4] = {c0[s].x, c0[s].y, c0[s].z, c0[s].w}, w1[4] = {c1[s].x, c1[s].y, c1[s].z, c1[s].w};
@@ -292,16 +296,12 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
                 }
             }
         };
-        for (int i = 0; i < per_unit;) {
+        for (int i = 0; i < padded; i += kAhead)
 #pragma unroll
-            for (int s = 0; s < kAhead; ++s)
-                if (s == slot && i < per_unit) {
-                    if (tile < p.tiles) block(s, i);
-                    load_next(s);
-                    ++i;
-                    slot = s + 1 == kAhead ? 0 : s + 1;
-                }
-        }
+            for (int s = 0; s < kAhead; ++s) {
+                if (i + s < per_unit && tile < p.tiles) block(s, i + s);
+                load_next(s);
+            }
         // ---- partial sums meet: [warp][row][token]
         float* red = s_red + warp * 16 * TN;
 #pragma unroll
@@ -405,8 +405,8 @@ constexpr size_t kMost = 200 * 1024;
 struct LinearPlan { int nt, wk, cluster, cta_blocks, grid; size_t smem; int64_t cost; };
 
 // Tokens of a pass (8 NT), warps that share a row tile, CTAs that share the input dimension: what takes the least by the rounds that a CTA's
-// warps make.  In clocks: a block of 128 codes 150 + 110 NT of a warp with seven beside it, the sums' meeting 700 + 60 NT and 1500 more in a
-// cluster, the activations 1500 + 60 NT a block at the start.
+// warps make.  In clocks: a block of 128 codes 200 + 100 NT of a warp with seven beside it and half as much more with fifteen, the sums' meeting
+// 700 + 60 NT and 1500 more in a cluster, the activations 1500 + 60 NT a block at the start.
 template <int GS, int NT> void plan_linear(const LinearParams& p, int sms, LinearPlan& best) {
     const int slices = (p.T + NT * 8 - 1) / (NT * 8);
     for (int c = 1; c <= 8; c *= 2)
@@ -419,11 +419,10 @@ template <int GS, int NT> void plan_linear(const LinearParams& p, int sms, Linea
             const int units = (p.tiles + kWarps / wk - 1) / (kWarps / wk), room = sms * resident / c > 0 ? sms * resident / c : 1;
             const int64_t all = (int64_t)units * slices, rounds = (all + room - 1) / room;
             const int beside = all * c > sms ? resident : 1;                           // CTAs that share an SM's pipes
-            const int64_t cost = rounds * ((int64_t)((each + wk - 1) / wk) * (150 + 110 * NT) * beside + 700 + 60 * NT + (c > 1 ? 1500 : 0)) +
-                                 (int64_t)(1500 + each * 60 * NT) * (slices > 1 ? (slices * c + sms - 1) / sms : 1);
+            const int64_t cost = rounds * ((int64_t)((each + wk - 1) / wk) * (200 + 100 * NT) * (beside > 1 ? 3 : 2) / 2 + 700 + 60 * NT + (c > 1 ? 1500 : 0)) +
+                                 1500 + each * 60 * NT;
             if (best.cost >= 0 && cost >= best.cost) continue;
-            const int waves = (units + room - 1) / room;
-            best = {NT, wk, c, each, (units + waves - 1) / waves, bytes, cost};
+            best = {NT, wk, c, each, (int)((units + rounds - 1) / rounds), bytes, cost};
         }
 }
 
