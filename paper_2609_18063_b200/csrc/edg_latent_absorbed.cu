@@ -60,7 +60,11 @@ __device__ __forceinline__ Seq sequence(const AbsorbedParams& p, int i) {
 }
 // places on the line that a unit takes: its tiles, behind kPiece that stand for what a piece costs beside them; and a group's share of a line of W
 __device__ __forceinline__ long long unit_length(const Seq& q) { return q.kt > 0 ? q.kt + kPiece : 0; }
-__device__ __forceinline__ long long stretch(long long W, int groups) { return (W + groups - 1) / groups; }
+// (quotients of 64 bits take some hundred clocks: nearly all fit 32)
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((a | b) >> 31) == 0 ? (long long)((unsigned)a / (unsigned)b) : a / b;
+}
+__device__ __forceinline__ long long stretch(long long W, int groups) { return quotient(W + groups - 1, groups); }
 
 // ---------------------------------------------------------------- queries to the latent space
 
@@ -298,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                 const Seq q = sequence(p, i);
                 const long long here = q.units * unit_length(q);
                 if (start < before + here) {
-                    const int ug = (int)((start - before) / unit_length(q));
+                    const int ug = (int)quotient(start - before, unit_length(q));
                     s_at[0] = i;
                     s_at[1] = ug;
                     s_at[2] = ub + ug;
@@ -470,11 +474,14 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                 const int row = wq * 16 + gq + 8 * i;
                 sees[i] = mine && row < w.rows ? min(w.q.len, w.q.len - w.q.fresh + (w.first_row + row) / p.heads + 1) : 0;
             }
-            for (int t = w.t0; t < w.t1; ++t, ++n) {
+            // (The first time round these warps go through the motions on whatever tensor memory holds, and forget it: the loads take longer than
+            // the fetching of this code, which took 4000 clocks of the first tile.)
+            for (int t = n == 0 ? w.t0 - 1 : w.t0; t < w.t1; ++t) {
                 const int buf = n & 1;
-                role_wait(&s_full[buf], (uint32_t)(n >> 1) & 1, p.status);
+                const bool dry = t < w.t0, first = t <= w.t0;
+                if (!dry) role_wait(&s_full[buf], (uint32_t)(n >> 1) & 1, p.status);
                 tc_fence_after();
-                const bool first = t == w.t0;
+                if (t == w.t0) { m[0] = m[1] = -INFINITY; l[0] = l[1] = 0.f; }
                 float s[2][16], mt[2] = {m[0], m[1]};
                 if (mine) {
                     uint32_t v[32];
@@ -505,7 +512,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&s_empty[buf]);
+                if (lane == 0 && !dry) mbar_arrive(&s_empty[buf]);
                 if (first) { m[0] = mt[0]; m[1] = mt[1]; }
                 const bool grown0 = mt[0] > m[0] + 8.f, grown1 = mt[1] > m[1] + 8.f;      // (-infinity: anything is more)
                 const bool rescale = barrier_or(1, 128, grown0 || grown1);
@@ -546,6 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                         l[i] += la + lb;
                     }
                 }
+                if (dry) continue;
                 const int held = w.q.len - t * 64;                       // positions of the tile that exist: clear the rows behind them
                 if (held < 64) {
                     RingAt c = vt;
@@ -577,6 +585,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                 fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full);
+                ++n;
             }
             // ---- the piece's sums
             role_wait(pv_done, (uint32_t)(n - 1) & 1, p.status);
@@ -616,24 +625,28 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
 constexpr int kCombine = 512;
 
 // A CTA: one head of 16 rows.  A warp adds up the pieces of a row and leaves its latent sums in shared memory as two bf16 parts, 16 bits of
-// them in all; then every warp takes eight values of W_uv, whose rows it has asked for before anything else.
+// them in all; then every warp takes 32 values of W_uv over a quarter of the latent columns, asked for before anything else (eight values over
+// all of them read the sums from shared memory four times as often: 5000 clocks instead of 1500).
 __global__ void __launch_bounds__(kCombine, 1) combine_kernel(const __grid_constant__ AbsorbedParams p) {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ float s_weight[16][kSms];
     __shared__ int s_row[16];                                           // new rows of this CTA, or -1
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
     const int h = blockIdx.x, t0 = blockIdx.y * 16, pitch = p.dl * 2 + 64, kb = p.dl / 32;
-    const bool values = warp * 8 < p.dv;
+    const int v0 = (warp & 3) * 32, quarter = warp >> 2, kq = kb / 4;    // (d_latent is a multiple of 128)
     const bool all = p.most >= p.max_new;
     if (!all) {
         pdl_wait_prior_grid();
         if (t0 >= p.row_pre[p.s.n]) return;
     }
     // lane t4 of a quad takes columns 8 t4 .. 8 t4 + 7 of every 32, of both operands: any order of k will do
-    uint4 w[16];
+    uint4 w[4][4];
 #pragma unroll
-    for (int k = 0; k < 16; ++k)
-        if (values && k < kb) w[k] = __ldg(reinterpret_cast<const uint4*>(p.W_uv + ((size_t)h * p.dv + warp * 8 + g) * p.dl + t4 * 8 + k * 32));
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (v0 + j * 8 < p.dv && k < kq)
+                w[j][k] = __ldg(reinterpret_cast<const uint4*>(p.W_uv + ((size_t)h * p.dv + v0 + j * 8 + g) * p.dl + t4 * 8 + (quarter * kq + k) * 32));
     pdl_wait_prior_grid();
     {
         int first = 0, count = 0, row = -1;
@@ -648,7 +661,7 @@ __global__ void __launch_bounds__(kCombine, 1) combine_kernel(const __grid_const
             row = (rt - ug * p.group) * p.R + in - rt * p.R;
             if (q.kt > 0) {
                 const long long each = stretch(W, p.groups), at = before + ug * unit_length(q) + kPiece;
-                const int g0 = (int)(at / each), g1 = (int)((at + q.kt - 1) / each);
+                const int g0 = (int)quotient(at, each), g1 = (int)quotient(at + q.kt - 1, each);
                 first = g0 + units + ug;
                 count = max(min(g1 - g0 + 1, p.max_slots - first), 0);
             }
@@ -703,28 +716,48 @@ __global__ void __launch_bounds__(kCombine, 1) combine_kernel(const __grid_const
             }
     }
     __syncthreads();
-    if (!values) return;
-    float d[4][4] = {};                                                  // (four chains of products, by part and half of a block)
-    const uint8_t* a0 = smem + g * pitch + t4 * 16;
+    float d[4][4] = {};
+    const uint8_t* a0 = smem + g * pitch + t4 * 16 + quarter * kq * 64;
 #pragma unroll
-    for (int k = 0; k < 16; ++k)
-        if (k < kb)
+    for (int k = 0; k < 4; ++k)
+        if (k < kq)
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
                 const uint8_t* a = a0 + part * 16 * pitch + k * 64;
                 const uint4 x = *reinterpret_cast<const uint4*>(a), z = *reinterpret_cast<const uint4*>(a + 8 * pitch);
-                mma16816_bf16(d[part * 2], x.x, z.x, x.y, z.y, w[k].x, w[k].y);
-                mma16816_bf16(d[part * 2 + 1], x.z, z.z, x.w, z.w, w[k].z, w[k].w);
-            }
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int t = s_row[g + 8 * e];
-        if (t < 0) continue;
-        const size_t at = ((size_t)t * p.heads + h) * p.dv + warp * 8 + 2 * t4;
-        const float x = (d[0][2 * e] + d[1][2 * e]) + (d[2][2 * e] + d[3][2 * e]), y = (d[0][2 * e + 1] + d[1][2 * e + 1]) + (d[2][2 * e + 1] + d[3][2 * e + 1]);
-        if (p.out_dtype == EDG_F16) *reinterpret_cast<__half2*>(static_cast<__half*>(p.y) + at) = __floats2half2_rn(x, y);
-        else *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.y) + at) = bf16_pair(x, y);
+                for (int j = 0; j < 4; ++j)
+                    if (v0 + j * 8 < p.dv) {
+                        mma16816_bf16(d[j], x.x, z.x, x.y, z.y, w[j][k].x, w[j][k].y);
+                        mma16816_bf16(d[j], x.z, z.z, x.w, z.w, w[j][k].z, w[j][k].w);
+                    }
+            }
+    // the quarters meet in shared memory: [quarter][row][value]
+    __syncthreads();
+    float* s_d = reinterpret_cast<float*>(smem);
+    constexpr int kRow = 132;                                            // floats of a row: 128 and padding
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float* out = s_d + (quarter * 16 + g) * kRow + v0 + j * 8 + 2 * t4;
+        *reinterpret_cast<float2*>(out) = make_float2(d[j][0], d[j][1]);
+        *reinterpret_cast<float2*>(out + 8 * kRow) = make_float2(d[j][2], d[j][3]);
     }
+    __syncthreads();
+    const int r = tid >> 5, v = lane * 4, t = s_row[r];
+    if (t < 0 || v >= p.dv) return;
+    float4 y = *reinterpret_cast<const float4*>(s_d + r * kRow + v);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+        const float4 x = *reinterpret_cast<const float4*>(s_d + (i * 16 + r) * kRow + v);
+        y.x += x.x; y.y += x.y; y.z += x.z; y.w += x.w;
+    }
+    const size_t at = ((size_t)t * p.heads + h) * p.dv + v;
+    uint2 o;
+    if (p.out_dtype == EDG_F16) {
+        const __half2 a = __floats2half2_rn(y.x, y.y), b = __floats2half2_rn(y.z, y.w);
+        o = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+    } else o = make_uint2(bf16_pair(y.x, y.y), bf16_pair(y.z, y.w));
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.y) + at) = o;
 }
 
 struct AbsorbedLayout { int R, group, groups, slots; size_t tile_pre, unit_pre, row_pre, q_lat, ml, part, bytes; };
@@ -814,7 +847,8 @@ int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new,
     EDG_CUDA_TRY(L.R == 16   ? launch_pdl(absorbed_kernel<16>, grid, kThreads, Plan<16>::bytes, st, p, kv_map, q_map)
                  : L.R == 32 ? launch_pdl(absorbed_kernel<32>, grid, kThreads, Plan<32>::bytes, st, p, kv_map, q_map)
                              : launch_pdl(absorbed_kernel<64>, grid, kThreads, Plan<64>::bytes, st, p, kv_map, q_map));
-    EDG_CUDA_TRY(launch_pdl(combine_kernel, dim3(d.heads, (unsigned)((rows + 15) / 16)), kCombine, (size_t)32 * (d.d_latent * 2 + 64), st, p));
+    EDG_CUDA_TRY(launch_pdl(combine_kernel, dim3(d.heads, (unsigned)((rows + 15) / 16)), kCombine,
+                            (size_t)(32 * (d.d_latent * 2 + 64) > 4 * 16 * 132 * 4 ? 32 * (d.d_latent * 2 + 64) : 4 * 16 * 132 * 4), st, p));
     return EDG_OK;
 }
 
