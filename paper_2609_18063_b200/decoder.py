@@ -1,4 +1,5 @@
-"""The expert stack: one token through L MoE layers with prediction-driven staging.
+"""The expert stack: one token through L MoE layers with prediction-driven staging; and whole decoder blocks, with
+latent attention over a paged cache in front of each layer-step.
 
 A thin owner of the buffers around ``edg_stack_decode_token`` -- the per-token host loop itself (wait
 for the mirrored routing, stage, enqueue the L layer-steps) runs inside the C library.  Per token
@@ -10,6 +11,8 @@ copies of the missing experts on the side stream, and each layer's kernel waits 
 layer's copies, so later layers' copies overlap earlier layers' compute.
 """
 from __future__ import annotations
+
+import time
 
 import torch
 
@@ -49,3 +52,112 @@ class StackDecoder:
         self.misses += B.stack_decode_token(self.store, X, self.inds[cur], self.gates[cur], self.W_pre,
                                             self.inds[nxt], self.gates[nxt], logits_out, self.mirror[cur],
                                             self.mirror[nxt], Y, self.ws, prefetch=self.prefetch)
+
+
+class LatentCache:
+    """Latent rows of all layers in pages, and which pages a request holds (device state, ``edg.pages_*``)."""
+
+    def __init__(self, layers: int, n_pages: int, page: int, row: int, n_seqs: int, max_pages: int, device="cuda"):
+        """row: d_latent + d_rope values of bf16."""
+        self.rows = torch.zeros((layers, n_pages, page, row), dtype=torch.bfloat16, device=device)
+        self.refs = torch.zeros(n_pages, dtype=torch.int32, device=device)
+        self.table = torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device)
+        self.lens = torch.zeros(n_seqs, dtype=torch.int32, device=device)
+        self.pool = B.make_page_pool(self.refs, self.table, self.lens, page=page)
+        self.pages = B.make_page_cache(self.rows)
+        self.ws = torch.zeros(B.pages_workspace_bytes(self.pool), dtype=torch.uint8, device=device)
+
+    def reserve(self, seqs: torch.Tensor, counts: torch.Tensor) -> None:
+        B.pages_reserve(self.pool, self.pages, seqs.numel(), seqs, counts, self.ws)
+
+    def fork(self, parents: torch.Tensor, children: torch.Tensor) -> None:
+        B.pages_fork(self.pool, parents.numel(), parents, children, self.ws)
+
+    def free(self, seqs: torch.Tensor) -> None:
+        B.pages_free(self.pool, seqs.numel(), seqs, self.ws)
+
+    def compact(self) -> None:
+        B.pages_compact(self.pool, self.pages, self.ws)
+
+    def status(self) -> int:
+        return B.workspace_status(self.ws)
+
+
+class LatentBlock:
+    """The attention half of one decoder layer: int4 projections of the hidden state to queries and latent rows, latent attention over the
+    request's pages, int4 output projection.  Serves single tokens, batches of requests and prompts alike.
+
+    ``w_q``, ``w_kv``, ``w_out``: (LinearDesc, device record) with N = heads * (d_nope + d_rope), d_latent + d_rope and H; ``w_uk`` / ``w_uv`` device
+    bf16 [heads][d_nope][d_latent] / [heads][d_v][d_latent]; ``gain`` device bf16 [d_latent] or None; ``inv_freq`` device f32 [d_rope / 2].
+    Adapters: an optional (A, B) behind the record."""
+
+    def __init__(self, desc: B.LatentDesc, w_q, w_kv, w_out, w_uk, w_uv, gain, inv_freq, max_rows: int, max_seqs: int, max_new: int, max_total: int):
+        self.desc, self.w_q, self.w_kv, self.w_out = desc, w_q, w_kv, w_out
+        self.w_uk, self.w_uv, self.gain, self.inv_freq = w_uk, w_uv, gain, inv_freq
+        h, dev = desc.heads, w_uk.device
+        half = {B.F16: torch.float16, B.BF16: torch.bfloat16}[desc.out_dtype]
+        self.q = torch.empty((max_rows, h * (desc.d_nope + desc.d_rope)), dtype=torch.bfloat16, device=dev)
+        self.kv = torch.empty((max_rows, desc.d_latent + desc.d_rope), dtype=torch.bfloat16, device=dev)
+        self.q_rope = torch.empty((max_rows, h, desc.d_rope), dtype=torch.bfloat16, device=dev)
+        self.a = torch.empty((max_rows, h * desc.d_v), dtype=half, device=dev)
+        self.bounds = (max_seqs, max_rows, max_new, max_total)
+        self.ws = torch.zeros(B.latent_workspace_bytes(desc, *self.bounds), dtype=torch.uint8, device=dev)
+        need = max(B.linear_workspace_bytes(w[0], max_rows) for w in (w_q, w_kv, w_out))
+        self.ws_linear = torch.empty(need, dtype=torch.uint8, device=dev)
+
+    def _project(self, w, T, x, y):
+        A, Bm = (w[2], w[3]) if len(w) > 2 else (None, None)
+        B.linear_int4_lora(w[0], w[1], T, x, A, Bm, y, self.ws_linear)
+
+    def run(self, x, y, cu, lens, table, rows, max_new=1, total=None, eps=1e-6) -> None:
+        """x device bf16 [T][H] (the new rows of n = cu.numel() - 1 sequences, whose places in the cache are reserved), y device [T][H] of
+        ``w_out``'s type; lens and table are those of the same n sequences, rows the layer's part of the cache; total bounds the sum of lens."""
+        n, T = cu.numel() - 1, x.shape[0]
+        total = self.bounds[3] if total is None else total
+        self._project(self.w_q, T, x, self.q)
+        self._project(self.w_kv, T, x, self.kv)
+        B.latent_append(self.desc, n, T, cu, lens, table, self.kv, self.gain, eps, self.inv_freq, self.q, self.q_rope, rows, self.ws)
+        B.latent_attention(self.desc, n, T, max_new, total, cu, lens, table, self.q, self.q_rope, self.w_uk, self.w_uv, rows, self.a, self.ws)
+        self._project(self.w_out, T, self.a, y)
+
+
+class BlockDecoder(StackDecoder):
+    """A request through a stack of whole decoder blocks: the attention half (:class:`LatentBlock`) in front of every MoE layer-step, the
+    hidden state handed on as bf16(rmsnorm(x + y)) behind each of the two.  Routing is predicted as in :class:`StackDecoder`: the head owned by
+    layer l, evaluated on that layer-step's input at token t, predicts layer (l + 1) % L at token t + 1."""
+
+    def __init__(self, desc: B.LayerDesc, store: B.Store, W_pre: torch.Tensor, blocks, cache: LatentCache, seq: int = 0):
+        super().__init__(desc, store, W_pre)
+        if len(blocks) != self.L or cache.rows.shape[0] != self.L:
+            raise ValueError("one attention block and one layer of the cache per layer of the store")
+        self.blocks, self.cache = blocks, cache
+        dev = W_pre.device
+        self._seq = torch.tensor([seq], dtype=torch.int32, device=dev)
+        self._one = torch.ones(1, dtype=torch.int32, device=dev)
+        self._cu = torch.tensor([0, 1], dtype=torch.int32, device=dev)
+        self._lens, self._table = cache.lens[seq:seq + 1], cache.table[seq:seq + 1]
+        dt = {B.F32: torch.float32, B.F16: torch.float16, B.BF16: torch.bfloat16}[desc.out_dtype]
+        self.o = torch.empty(desc.H, dtype=dt, device=dev)              # attention output, of the type that the next state is made from
+        self.y = torch.empty((self.L, desc.H), dtype=dt, device=dev)
+        self.x_moe = torch.empty((self.L, desc.H), dtype=torch.bfloat16, device=dev)
+        self.x_out = torch.empty((self.L, desc.H), dtype=torch.bfloat16, device=dev)
+
+    def token(self, t: int, x: torch.Tensor, timeout_s: float = 5.0) -> torch.Tensor:
+        """Token t: x device bf16 [H], the first block's input; returns the last block's output (a view that the next token overwrites)."""
+        cur, nxt = t % 2, (t + 1) % 2
+        mirror, end = self.mirror[cur].numpy(), time.monotonic() + timeout_s
+        while (mirror < 0).any():                                       # written by the heads of the token before
+            if time.monotonic() > end:
+                raise B.EdgError(-6, "BlockDecoder.token")
+        self.mirror[nxt].fill_(-1)
+        for l in range(self.L):
+            self.misses += B.stage_experts_to_slots(self.store, l, mirror[l])[1]
+        self.cache.reserve(self._seq, self._one)
+        for l, block in enumerate(self.blocks):
+            block.run(x.view(1, -1), self.o, self._cu, self._lens, self._table, self.cache.rows[l])
+            B.next_hidden_state(self.desc, x, self.o, self.x_moe[l])
+            nl = (l + 1) % self.L
+            B.moe_layer_decode_dependent(self.store, l, self.x_moe[l], self.inds[cur][l], self.gates[cur][l], self.W_pre[l], self.inds[nxt][nl],
+                                         self.gates[nxt][nl], None, self.y[l], self.x_out[l], self.ws, inds_next_host_mirror_opt=self.mirror[nxt][nl])
+            x = self.x_out[l]
+        return x
