@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(128) absorb_kernel(const __grid_constant__ Abs
 
 // ---------------------------------------------------------------- attention over pieces
 
-constexpr int kThreads = 256;               // warps 0 and 3 load, 1 and 2 issue products, 4-7 softmax and epilogue
+constexpr int kThreads = 384;               // warps 0 and 3 load, 1 and 2 issue products, 4-11 softmax and epilogue
 constexpr uint32_t kUnit = 16384, kRope = 8192;      // 64 positions x 128 latent columns; x 64 rotated ones
 
 constexpr int kFull = 4;                    // "tile is there" barriers: more than tiles that fit the ring of rotated parts
@@ -196,7 +196,7 @@ constexpr int kFull = 4;                    // "tile is there" barriers: more th
 template <int R> struct Plan {
     static constexpr int NV = R == 64 ? 8 : (R == 32 ? 10 : 11), NR = R == 64 ? 2 : 3;
     static constexpr uint32_t q = 0, p = 9 * R * 128, rope = p + R * 128, unit = rope + NR * kRope, bars = unit + NV * kUnit;
-    static constexpr uint32_t alpha = bars + (NV + NR + kFull + 12) * 8, end = alpha + 64 * 4 + 64, bytes = end + 1024;
+    static constexpr uint32_t alpha = bars + (NV + NR + 2 * kFull + 12) * 8, most = alpha + 64 * 4, end = most + 2 * 2 * 64 * 4, bytes = end + 1024;
     static constexpr uint32_t columns = R == 64 ? 512 : 256;            // of tensor memory: S twice 64, O 4 R
     static_assert(bytes <= 227 * 1024, "shared memory");
     static_assert(p % 1024 == 0 && rope % 1024 == 0 && unit % 1024 == 0, "swizzle atoms");
@@ -239,8 +239,8 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
     const uint32_t sb = smem_u32(smem);
     uint64_t* v_empty = reinterpret_cast<uint64_t*>(smem + P::bars);     // [NV]
     uint64_t* r_empty = v_empty + P::NV;                                 // [NR]
-    uint64_t* t_full = r_empty + P::NR;                                  // [kFull]
-    uint64_t* q_full = t_full + kFull;
+    uint64_t* t_full = r_empty + P::NR;                                  // [kFull][2]: rotated parts and the first half of the units, the others
+    uint64_t* q_full = t_full + 2 * kFull;
     uint64_t* q_empty = q_full + 1;
     uint64_t* s_full = q_empty + 1;                                      // [2]
     uint64_t* s_empty = s_full + 2;                                      // [2]
@@ -249,6 +249,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
     uint64_t* o_empty = pv_done + 1;
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(o_empty + 1);
     float* s_alpha = reinterpret_cast<float*>(smem + P::alpha);
+    float* s_most = reinterpret_cast<float*>(smem + P::most);             // [2][half of the columns][row]
     __shared__ long long s_tiles[kThreads / 32], s_from[2];
     __shared__ int s_units[kThreads / 32], s_at[3];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -256,13 +257,13 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
     if (tid == 0) {
         for (int i = 0; i < P::NV; ++i) mbar_init(&v_empty[i], 1);
         for (int i = 0; i < P::NR; ++i) mbar_init(&r_empty[i], 1);
-        for (int i = 0; i < kFull; ++i) mbar_init(&t_full[i], 1);
+        for (int i = 0; i < 2 * kFull; ++i) mbar_init(&t_full[i], 1);
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&s_empty[i], 4); }
-        mbar_init(p_full, 4);
+        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&s_empty[i], 8); }
+        mbar_init(p_full, 8);
         mbar_init(pv_done, 1);
-        mbar_init(o_empty, 4);
+        mbar_init(o_empty, 8);
         fence_barrier_init();
     }
     if (warp == 1) tmem_alloc(s_tmem, P::columns);
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
     w.tile = (int)s_from[0];
     w.left = s_from[1];
     const uint32_t tmem = *s_tmem;
-    const int NU = p.dl / 128;
+    const int NU = p.dl / 128, n1 = (NU + 1) / 2;                        // units of 128 columns; the first half of them
 
     if (warp == 0 || warp == 3) {
         // ============================================= loads: warp 0 takes the first 64 columns of every unit, the rotated parts and Q, warp 3 the
@@ -351,10 +352,11 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                 for (int b = 0; b < 4; ++b) y[b] = __shfl_sync(0xFFFFFFFFu, coord, (t * boxes - base + min(b, boxes - 1)) & 31);
                 role_wait(&r_empty[ro.slot], ro.phase ^ 1, p.status);
                 if (half == 0 && elected()) {
-                    mbar_expect_tx(&t_full[f.slot], kRope + NU * kUnit);
+                    mbar_expect_tx(&t_full[2 * f.slot], kRope + n1 * kUnit);
+                    if (n1 < NU) mbar_expect_tx(&t_full[2 * f.slot + 1], (NU - n1) * kUnit);
 #pragma unroll
                     for (int b = 0; b < 4; ++b)
-                        if (b < boxes) tma_2d(sb + P::rope + ro.slot * kRope + b * br * 128, &kv_map, p.dl, y[b], &t_full[f.slot]);
+                        if (b < boxes) tma_2d(sb + P::rope + ro.slot * kRope + b * br * 128, &kv_map, p.dl, y[b], &t_full[2 * f.slot]);
                 }
                 ro.next(P::NR);
                 for (int u = 0; u < NU; ++u) {
@@ -362,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                     if (elected()) {
 #pragma unroll
                         for (int b = 0; b < 4; ++b)
-                            if (b < boxes) tma_2d(sb + P::unit + v.slot * kUnit + half * kRope + b * br * 128, &kv_map, u * 128 + half * 64, y[b], &t_full[f.slot]);
+                            if (b < boxes) tma_2d(sb + P::unit + v.slot * kUnit + half * kRope + b * br * 128, &kv_map, u * 128 + half * 64, y[b], &t_full[2 * f.slot + (u >= n1)]);
                     }
                     v.next(P::NV);
                 }
@@ -381,8 +383,8 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
         }
         if (!waited) pdl_wait_prior_grid();
     } else if (warp == 1) {
-        // ============================================= S of every tile.  All that it needs is waited for before the first of its products:
-        // a wait between two of them costs as much as four of them.  (And O is another warp's, whose waits these products cover.)
+        // ============================================= S of every tile, in two halves as they arrive.  (O is another warp's: what queues up
+        // behind a product covers two or three of them, a wait costs as much, and each warp's products cover the other's waits.)
         const uint32_t id_s = idesc_bf16(64, 64);
         const uint32_t dq = desc_lo(sb + P::q), dk0 = desc_lo(sb + P::unit), dr0 = desc_lo(sb + P::rope);
         const int rks = p.dr / 16;
@@ -395,8 +397,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
             for (int t = w.t0; t < w.t1; ++t, ++n) {
                 const int buf = n & 1;
                 role_wait(&s_empty[buf], ((uint32_t)(n >> 1) & 1) ^ 1, p.status);
-                role_wait(&t_full[f.slot], f.phase, p.status);
-                f.next(kFull);
+                role_wait(&t_full[2 * f.slot], f.phase, p.status);
                 uint32_t at[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
@@ -408,19 +409,37 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                 const uint32_t d = tmem + buf * 64, dr = dr0 + ((kr.slot * kRope) >> 4);
                 if (elected()) {
 #pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        if (u < NU)
+                    for (int k = 0; k < 4; ++k)
+                        if (k < rks) umma_ss(d, dq + ((NU * 2 * R * 128 + k * 32) >> 4), dr + ((k * 32) >> 4), id_s, k > 0);
+                    umma_done(&r_empty[kr.slot]);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+                        if (u < n1)
 #pragma unroll
                             for (int k = 0; k < 8; ++k)
-                                umma_ss(d, dq + (((u * 2 + (k >> 2)) * R * 128 + (k & 3) * 32) >> 4), at[u] + (((k >> 2) * kRope + (k & 3) * 32) >> 4), id_s, u + k > 0);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (k < rks) umma_ss(d, dq + ((NU * 2 * R * 128 + k * 32) >> 4), dr + ((k * 32) >> 4), id_s, true);
-                    umma_done(&s_full[buf]);
-                    umma_done(&r_empty[kr.slot]);
-                    if (t == w.t1 - 1) umma_done(q_empty);
+                                umma_ss(d, dq + (((u * 2 + (k >> 2)) * R * 128 + (k & 3) * 32) >> 4), at[u] + (((k >> 2) * kRope + (k & 3) * 32) >> 4), id_s, true);
+                    if (n1 == NU) {
+                        umma_done(&s_full[buf]);
+                        if (t == w.t1 - 1) umma_done(q_empty);
+                    }
                 }
                 __syncwarp();
+                if (n1 < NU) {
+                    role_wait(&t_full[2 * f.slot + 1], f.phase, p.status);
+                    tc_fence_after();
+                    if (elected()) {
+#pragma unroll
+                        for (int u = 1; u < 4; ++u)
+                            if (u >= n1 && u < NU)
+#pragma unroll
+                                for (int k = 0; k < 8; ++k)
+                                    umma_ss(d, dq + (((u * 2 + (k >> 2)) * R * 128 + (k & 3) * 32) >> 4), at[u] + (((k >> 2) * kRope + (k & 3) * 32) >> 4), id_s, true);
+                        umma_done(&s_full[buf]);
+                        if (t == w.t1 - 1) umma_done(q_empty);
+                    }
+                    __syncwarp();
+                }
+                f.next(kFull);
                 kr.next(P::NR);
             }
         }
@@ -459,12 +478,12 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
     } else if (warp >= 4) {
         // ============================================= softmax, rescaling, epilogue
         // A product of M = 64 leaves its rows in 16 lanes of every 32; a load of that shape gives a lane two rows (gq, gq + 8 of the warp's
-        // 16), and of them the columns 8 j + 2 cq and the next.
-        const int wq = warp & 3, gq = lane >> 2, cq = lane & 3;
+        // 16), and of them the columns 8 j + 2 cq and the next.  Two warps share the rows, 32 columns each.
+        const int wq = warp & 3, half = (warp >> 2) - 1, gq = lane >> 2, cq = lane & 3;
         const bool mine = wq * 16 < R;
         const uint32_t lanes = (uint32_t)(wq * 32) << 16;
         const float k2 = p.scale * 1.4426950408889634f;
-        RingAt vt;                                                       // units of the tile at hand (to clear rows behind the end)
+        RingAt vn;                                                       // units of the next tile (to clear rows behind the end)
         int n = 0;
         while (w.next(p, g, r)) {
             float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};      // (l: this lane's share)
@@ -482,49 +501,56 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                 if (!dry) role_wait(&s_full[buf], (uint32_t)(n >> 1) & 1, p.status);
                 tc_fence_after();
                 if (t == w.t0) { m[0] = m[1] = -INFINITY; l[0] = l[1] = 0.f; }
-                float s[2][16], mt[2] = {m[0], m[1]};
+                float s[2][8], mt[2] = {-INFINITY, -INFINITY};
                 if (mine) {
-                    uint32_t v[32];
-                    tmem_ld_rows16(tmem + lanes + buf * 64, v);
+                    uint32_t v[16];
+                    tmem_ld_rows16(tmem + lanes + buf * 64 + half * 32, v);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const int seen = sees[i] - t * 64 - 2 * cq;
-                        float a = -INFINITY, b = -INFINITY;
+                        const int seen = sees[i] - t * 64 - half * 32 - 2 * cq;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
+                        for (int j = 0; j < 4; ++j) {
                             s[i][2 * j] = __uint_as_float(v[4 * j + 2 * i]) * k2;
                             s[i][2 * j + 1] = __uint_as_float(v[4 * j + 2 * i + 1]) * k2;
                         }
-                        if (seen < 58) {                                 // (the last two of the lane's columns are 56 and 57 from its first)
+                        if (seen < 26) {                                 // (the last two of the lane's columns are 24 and 25 from its first)
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
+                            for (int j = 0; j < 4; ++j) {
                                 if (8 * j >= seen) s[i][2 * j] = -INFINITY;
                                 if (8 * j + 1 >= seen) s[i][2 * j + 1] = -INFINITY;
                             }
                         }
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) { a = fmaxf(a, s[i][2 * j]); b = fmaxf(b, s[i][2 * j + 1]); }
-                        a = fmaxf(a, b);
+                        float a = fmaxf(fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3])), fmaxf(fmaxf(s[i][4], s[i][5]), fmaxf(s[i][6], s[i][7])));
                         a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
-                        a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
-                        mt[i] = fmaxf(mt[i], a);
+                        mt[i] = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
+                    }
+                    if (cq == 0) {
+                        s_most[(buf * 2 + half) * 64 + wq * 16 + gq] = mt[0];
+                        s_most[(buf * 2 + half) * 64 + wq * 16 + gq + 8] = mt[1];
                     }
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0 && !dry) mbar_arrive(&s_empty[buf]);
-                if (first) { m[0] = mt[0]; m[1] = mt[1]; }
-                const bool grown0 = mt[0] > m[0] + 8.f, grown1 = mt[1] > m[1] + 8.f;      // (-infinity: anything is more)
-                const bool rescale = barrier_or(1, 128, grown0 || grown1);
+                // One barrier brings the other half's maxima and whether any row has grown (which either half of it tells).  A tile later the
+                // maxima go to the other buffer, and nobody is two tiles ahead: the barrier again.
+                const bool rescale = barrier_or(1, 256, !first && (mt[0] > m[0] + 8.f || mt[1] > m[1] + 8.f)) && !first;      // (-infinity: anything is more)
+                if (first || rescale) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        if (mine) mt[i] = fmaxf(mt[i], s_most[(buf * 2 + 1 - half) * 64 + wq * 16 + gq + 8 * i]);
+                    if (first) { m[0] = mt[0]; m[1] = mt[1]; }
+                }
                 if (n > 0) role_wait(pv_done, (uint32_t)(n - 1) & 1, p.status);       // O is complete, P has been read
                 if (rescale) {
+                    const bool grown0 = mt[0] > m[0] + 8.f, grown1 = mt[1] > m[1] + 8.f;
                     const float a0 = grown0 ? exp2_approx(m[0] - mt[0]) : 1.f, a1 = grown1 ? exp2_approx(m[1] - mt[1]) : 1.f;
                     if (grown0) { m[0] = mt[0]; l[0] *= a0; }
                     if (grown1) { m[1] = mt[1]; l[1] *= a1; }
-                    if (mine && cq == 0) { s_alpha[wq * 16 + gq] = a0; s_alpha[wq * 16 + gq + 8] = a1; }
-                    barrier_sync(1, 128);
+                    if (mine && cq == 0 && half == 0) { s_alpha[wq * 16 + gq] = a0; s_alpha[wq * 16 + gq + 8] = a1; }
+                    barrier_sync(1, 256);
                     tc_fence_after();
-                    for (int u = 0; u < NU; ++u)
+                    for (int u = half; u < NU; u += 2)
 #pragma unroll
                         for (int c = 0; c < R; c += 16) {
                             uint32_t v[16];
@@ -544,22 +570,25 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                         uint8_t* out = smem + P::p + row * 128 + cq * 4;
                         float la = 0.f, lb = 0.f;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {                    // two positions to a word, under the swizzle
+                        for (int j = 0; j < 4; ++j) {                    // two positions to a word, under the swizzle
                             const uint32_t o = bf16_pair(exp2_approx(s[i][2 * j] - mm), exp2_approx(s[i][2 * j + 1] - mm));
                             la += bf16_lo(o);                            // (what the product sums)
                             lb += bf16_hi(o);
-                            *reinterpret_cast<uint32_t*>(out + ((j ^ (row & 7)) * 16)) = o;
+                            *reinterpret_cast<uint32_t*>(out + (((j + half * 4) ^ (row & 7)) * 16)) = o;
                         }
                         l[i] += la + lb;
                     }
                 }
                 if (dry) continue;
                 const int held = w.q.len - t * 64;                       // positions of the tile that exist: clear the rows behind them
+                const RingAt vt = vn;
+                vn.slot += NU;
+                if (vn.slot >= P::NV) vn.slot -= P::NV;
                 if (held < 64) {
                     RingAt c = vt;
                     for (int u = 0; u < NU; ++u) {
                         uint8_t* unit = smem + P::unit + c.slot * kUnit;
-                        for (int i = held * 8 + (tid - 128); i < 512; i += 128) {
+                        for (int i = held * 8 + (tid - 128); i < 512; i += 256) {
                             *reinterpret_cast<uint4*>(unit + i * 16) = make_uint4(0, 0, 0, 0);
                             *reinterpret_cast<uint4*>(unit + kRope + i * 16) = make_uint4(0, 0, 0, 0);
                         }
@@ -570,7 +599,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                 // must not reach the others by their weight of zero.
                 const int own = max(w.q.len - w.q.fresh + 1 - t * 64, 0);
                 if (own < min(held, 64))
-                    for (int i = own + wq; i < min(held, 64); i += 4) {
+                    for (int i = own + warp - 4; i < min(held, 64); i += 8) {
                         uint32_t most = 0;
                         RingAt c = vt;
                         for (int u = 0; u < NU; ++u, c.next(P::NV))
@@ -581,7 +610,6 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                                 if (lane < 16) *reinterpret_cast<uint4*>(smem + P::unit + c.slot * kUnit + (lane >> 3) * kRope + i * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
                         }
                     }
-                for (int u = 0; u < NU; ++u) vt.next(P::NV);
                 fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full);
@@ -592,13 +620,21 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
             tc_fence_after();
             const bool fits = w.slot < p.max_slots;
             const size_t at = ((size_t)w.slot * p.group + r) * R;
+            // (the other half's sums by way of the maxima's place: the buffer that the last tile did not use, and the next will)
+            float* shared = s_most + (n & 1) * 128;
+            float sum[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float sum = group_sum<4>(l[i]);
-                const int row = wq * 16 + gq + 8 * i;
-                if (fits && cq == 0 && mine && row < w.rows) p.ml[at + row] = make_float2(m[i], sum);
+                sum[i] = group_sum<4>(l[i]);
+                if (half == 1 && mine && cq == 0) shared[wq * 16 + gq + 8 * i] = sum[i];
             }
-            for (int u = 0; u < NU; ++u)
+            barrier_sync(1, 256);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = wq * 16 + gq + 8 * i;
+                if (fits && half == 0 && cq == 0 && mine && row < w.rows) p.ml[at + row] = make_float2(m[i], sum[i] + shared[row]);
+            }
+            for (int u = half; u < NU; u += 2)
 #pragma unroll
                 for (int c = 0; c < R; c += 16) {
                     uint32_t v[16];
@@ -608,6 +644,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                         for (int j = 0; j < 16; ++j)
                             if (c + j < w.rows) p.part[(at + c + j) * p.dl + u * 128 + wq * 32 + lane] = __uint_as_float(v[j]);
                 }
+            barrier_sync(1, 256);                                        // (read before the next tile's maxima)
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(o_empty);

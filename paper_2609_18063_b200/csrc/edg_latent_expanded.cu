@@ -88,9 +88,9 @@ __global__ void __launch_bounds__(256) prompt_plan_kernel(const __grid_constant_
 // ---------------------------------------------------------------- keys and values
 
 constexpr int kXThreads = 256;              // warp 0 loads, warp 1 issues products, warps 4-7 write out
-constexpr int kXRing = 3;                   // stages of 128 columns: with one chunk a stage, waits took as long as products
+constexpr int kXRing = 6;                   // chunks of weights in flight: as many as fit, a copy takes as long as five products of them
 constexpr uint32_t kChunk = 16384;          // 128 rows of 64 columns
-constexpr uint32_t kXW = 8 * kChunk, kXBars = kXW + kXRing * 2 * kChunk, kXBytes = kXBars + 256 + 1024;
+constexpr uint32_t kXW = 8 * kChunk, kXBars = kXW + kXRing * kChunk, kXBytes = kXBars + 256 + 1024;
 
 __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_constant__ ExpandedParams p, const __grid_constant__ CUtensorMap c_map,
                                                               const __grid_constant__ CUtensorMap uk_map, const __grid_constant__ CUtensorMap uv_map) {
@@ -145,13 +145,12 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
             RingAt w;
             for (int h = h0; h < h1; ++h)
                 for (int kv = 0; kv < 2; ++kv)
-                    for (int c = 0; c < nc; c += 2) {
+                    for (int c = 0; c < nc; ++c) {
                         role_wait(&w_empty[w.slot], w.phase ^ 1, p.status);
                         if (elected()) {
                             const int n = kv == 0 ? p.dn : p.dv;
-                            tma_2d(sb + kXW + w.slot * 2 * kChunk, kv == 0 ? &uk_map : &uv_map, c * 64, h * n, &w_full[w.slot]);
-                            tma_2d(sb + kXW + w.slot * 2 * kChunk + kChunk, kv == 0 ? &uk_map : &uv_map, c * 64 + 64, h * n, &w_full[w.slot]);
-                            mbar_expect_tx(&w_full[w.slot], n * 256);
+                            tma_2d(sb + kXW + w.slot * kChunk, kv == 0 ? &uk_map : &uv_map, c * 64, h * n, &w_full[w.slot]);
+                            mbar_expect_tx(&w_full[w.slot], n * 128);
                         }
                         __syncwarp();
                         w.next(kXRing);
@@ -165,16 +164,15 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
                 for (int kv = 0; kv < 2; ++kv, ++j) {
                     const uint32_t id = idesc_bf16(128, kv == 0 ? p.dn : p.dv), d = tmem + (j & 1) * 128;
                     role_wait(&d_empty[j & 1], ((uint32_t)(j >> 1) & 1) ^ 1, p.status);
-                    for (int c = 0; c < nc; c += 2) {
+                    for (int c = 0; c < nc; ++c) {
                         role_wait(&w_full[w.slot], w.phase, p.status);
                         tc_fence_after();
                         if (elected()) {
+                            const uint32_t a = dc + ((c * kChunk) >> 4), b = dw + ((w.slot * kChunk) >> 4);
 #pragma unroll
-                            for (int k = 0; k < 8; ++k)
-                                umma_ss(d, dc + (((c + (k >> 2)) * kChunk + (k & 3) * 32) >> 4), dw + ((w.slot * 2 * kChunk + (k >> 2) * kChunk + (k & 3) * 32) >> 4), id,
-                                        c + k > 0);
+                            for (int k = 0; k < 4; ++k) umma_ss(d, a + k * 2, b + k * 2, id, c + k > 0);
                             umma_done(&w_empty[w.slot]);
-                            if (c == nc - 2) umma_done(&d_full[j & 1]);
+                            if (c == nc - 1) umma_done(&d_full[j & 1]);
                         }
                         __syncwarp();
                         w.next(kXRing);
