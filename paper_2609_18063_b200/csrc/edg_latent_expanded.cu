@@ -88,10 +88,12 @@ __global__ void __launch_bounds__(256) prompt_plan_kernel(const __grid_constant_
 // ---------------------------------------------------------------- keys and values
 
 constexpr int kXThreads = 256;              // warp 0 loads, warp 1 issues products, warps 4-7 write out
-constexpr int kXRing = 6;                   // chunks of weights in flight: as many as fit, a copy takes as long as five products of them
+constexpr int kXRing = 12;                  // chunks of weights in flight: four behind the cache rows, eight where these lay
 constexpr uint32_t kChunk = 16384;          // 128 rows of 64 columns
-constexpr uint32_t kXW = 8 * kChunk, kXBars = kXW + kXRing * kChunk, kXBytes = kXBars + 256 + 1024;
+constexpr uint32_t kXOut = 12 * kChunk, kXBars = kXOut + 4 * 8192, kXBytes = kXBars + 256 + 1024;
 
+// The cache rows are the A operand of all products of a CTA.  They go on to tensor memory (256 columns of it): with both operands in shared
+// memory the products take all of its 128 bytes a clock, and the arrival of the weights comes on top (7,500 rows, 32 heads of 128: 88 us, and 69 from here).
 __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_constant__ ExpandedParams p, const __grid_constant__ CUtensorMap c_map,
                                                               const __grid_constant__ CUtensorMap uk_map, const __grid_constant__ CUtensorMap uv_map) {
     extern __shared__ uint8_t smem_raw[];
@@ -100,17 +102,19 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
     uint64_t* w_full = reinterpret_cast<uint64_t*>(smem + kXBars);       // [kXRing]
     uint64_t* w_empty = w_full + kXRing;
     uint64_t* c_full = w_empty + kXRing;
-    uint64_t* d_full = c_full + 1;                                       // [2]
+    uint64_t* a_full = c_full + 1;                                       // the cache rows are in tensor memory
+    uint64_t* d_full = a_full + 1;                                       // [2]
     uint64_t* d_empty = d_full + 2;                                      // [2]
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(d_empty + 2);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         for (int i = 0; i < kXRing; ++i) { mbar_init(&w_full[i], 1); mbar_init(&w_empty[i], 1); }
         mbar_init(c_full, 1);
+        mbar_init(a_full, 4);
         for (int i = 0; i < 2; ++i) { mbar_init(&d_full[i], 1); mbar_init(&d_empty[i], 4); }
         fence_barrier_init();
     }
-    if (warp == 1) tmem_alloc(s_tmem, 256);
+    if (warp == 1) tmem_alloc(s_tmem, 512);
     pdl_launch_dependents();
     pdl_wait_prior_grid();
     tc_fence_before();
@@ -121,6 +125,7 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
     const int h0 = (int)((int64_t)p.heads * split / p.splits), h1 = (int)((int64_t)p.heads * (split + 1) / p.splits);
     const bool there = tile < p.kv_pre[p.s.n] && (tile + 1) * 128 <= p.rows;
     const int nc = p.dl / 64;
+    auto chunk_at = [](int slot) { return (uint32_t)(slot < 4 ? slot + 8 : slot - 4) * kChunk; };      // (the cache rows come to chunks 0-7)
     if (there) {
         const int seq = find_sequence(p.kv_pre, p.s.n, tile, lane);
         const XSeq q = xsequence(p, seq);
@@ -143,23 +148,25 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
                 __syncwarp();
             }
             RingAt w;
+            bool moved = false;
             for (int h = h0; h < h1; ++h)
                 for (int kv = 0; kv < 2; ++kv)
                     for (int c = 0; c < nc; ++c) {
                         role_wait(&w_empty[w.slot], w.phase ^ 1, p.status);
+                        if (w.slot >= 4 && !moved) { role_wait(a_full, 0, p.status); moved = true; }
                         if (elected()) {
                             const int n = kv == 0 ? p.dn : p.dv;
-                            tma_2d(sb + kXW + w.slot * kChunk, kv == 0 ? &uk_map : &uv_map, c * 64, h * n, &w_full[w.slot]);
+                            tma_2d(sb + chunk_at(w.slot), kv == 0 ? &uk_map : &uv_map, c * 64, h * n, &w_full[w.slot]);
                             mbar_expect_tx(&w_full[w.slot], n * 128);
                         }
                         __syncwarp();
                         w.next(kXRing);
                     }
         } else if (warp == 1) {
-            const uint32_t dc = desc_lo(sb), dw = desc_lo(sb + kXW);
+            const uint32_t dw = desc_lo(sb);
             RingAt w;
             int j = 0;
-            role_wait(c_full, 0, p.status);
+            role_wait(a_full, 0, p.status);
             for (int h = h0; h < h1; ++h)
                 for (int kv = 0; kv < 2; ++kv, ++j) {
                     const uint32_t id = idesc_bf16(128, kv == 0 ? p.dn : p.dv), d = tmem + (j & 1) * 128;
@@ -168,9 +175,9 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
                         role_wait(&w_full[w.slot], w.phase, p.status);
                         tc_fence_after();
                         if (elected()) {
-                            const uint32_t a = dc + ((c * kChunk) >> 4), b = dw + ((w.slot * kChunk) >> 4);
+                            const uint32_t a = tmem + 256 + c * 32, b = dw + (chunk_at(w.slot) >> 4);
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) umma_ss(d, a + k * 2, b + k * 2, id, c + k > 0);
+                            for (int k = 0; k < 4; ++k) umma_ts(d, a + k * 8, b + k * 2, id, c + k > 0);
                             umma_done(&w_empty[w.slot]);
                             if (c == nc - 1) umma_done(&d_full[j & 1]);
                         }
@@ -186,9 +193,20 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
             // it stay what they are (their weight of zero times NaN would not).
             uint32_t most = 0;
             role_wait(c_full, 0, p.status);
-            for (int c = 0; c < nc; ++c)
+            for (int c = 0; c < nc; ++c) {
+                uint32_t v[32];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) most = bf16_magnitudes(most, *reinterpret_cast<const uint4*>(smem + c * kChunk + row * 128 + j * 16));
+                for (int j = 0; j < 8; ++j) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(smem + c * kChunk + row * 128 + ((j ^ (row & 7)) * 16));
+                    most = bf16_magnitudes(most, x);
+                    v[4 * j] = x.x; v[4 * j + 1] = x.y; v[4 * j + 2] = x.z; v[4 * j + 3] = x.w;
+                }
+                tmem_st(tmem + lanes + 256 + c * 32, v);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(a_full);
             const bool finite = !bf16_not_finite(most);
             if (split == 0) {                                            // the rotated part of this thread's row
                 uint4* out = reinterpret_cast<uint4*>(p.Rp + ((size_t)tile * 128 + row) * 64);
@@ -206,7 +224,7 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
                 for (int kv = 0; kv < 2; ++kv, ++j) {
                     const int n = kv == 0 ? p.dn : p.dv;
                     const bool keep = held && (kv == 0 || finite);
-                    uint16_t* out = (kv == 0 ? p.K : p.V) + ((size_t)h * p.rows + (size_t)tile * 128 + row) * n;
+                    uint8_t* stage = smem + kXOut + wq * 8192;
                     role_wait(&d_full[j & 1], (uint32_t)(j >> 1) & 1, p.status);
                     tc_fence_after();
 #pragma unroll 2
@@ -216,19 +234,29 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
                         uint32_t o[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) o[i] = keep ? bf16_pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])) : 0u;
-                        *reinterpret_cast<uint4*>(out + c) = make_uint4(o[0], o[1], o[2], o[3]);
-                        *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+                            *reinterpret_cast<uint4*>(stage + lane * 256 + (((c / 8 + x) ^ (lane & 7)) * 16)) = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
                     }
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&d_empty[j & 1]);
+                    // (the 32 rows lie one behind another: whole lines, by way of shared memory; a row's own thread wrote 16 bytes to each of 32 lines)
+                    uint16_t* out = (kv == 0 ? p.K : p.V) + ((size_t)h * p.rows + (size_t)tile * 128 + wq * 32) * n;
+                    const int pieces = n / 8;
+#pragma unroll 4
+                    for (int x = lane; x < 32 * pieces; x += 32) {
+                        const int rr = x / pieces, c = x - rr * pieces;
+                        *reinterpret_cast<uint4*>(out + (size_t)x * 8) = *reinterpret_cast<const uint4*>(stage + rr * 256 + ((c ^ (rr & 7)) * 16));
+                    }
+                    __syncwarp();
                 }
         }
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 1) tmem_free(tmem, 256);
+    if (warp == 1) tmem_free(tmem, 512);
 }
 
 // ---------------------------------------------------------------- attention
