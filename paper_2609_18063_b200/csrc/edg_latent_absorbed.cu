@@ -801,7 +801,7 @@ struct AbsorbedLayout { int R, group, groups, slots; size_t tile_pre, unit_pre, 
 
 AbsorbedLayout absorbed_layout(const edg_latent_desc& d, int n_seqs, int T, int max_new) {
     AbsorbedLayout L;
-    const int64_t rows = (int64_t)max_new * d.heads, all = (int64_t)T * d.heads;
+    const int64_t rows = (int64_t)max_new * d.heads, taken = (int64_t)n_seqs * max_new, all = (taken < T ? taken : T) * d.heads;
     L.R = absorbed_rows(rows);
     const int64_t tiles = (rows + L.R - 1) / L.R;
     L.group = (int)(tiles < kGroupMost ? tiles : kGroupMost);
@@ -814,7 +814,7 @@ AbsorbedLayout absorbed_layout(const edg_latent_desc& d, int n_seqs, int T, int 
     L.unit_pre = round_up(L.tile_pre + ((size_t)n_seqs + 1) * 8, 256);
     L.row_pre = round_up(L.unit_pre + ((size_t)n_seqs + 1) * 4, 256);
     L.q_lat = round_up(L.row_pre + ((size_t)n_seqs + 1) * 4, 256);
-    L.ml = round_up(L.q_lat + (size_t)all * (d.d_latent + 64) * 2, 256);
+    L.ml = round_up(L.q_lat + (size_t)T * d.heads * (d.d_latent + 64) * 2, 256);
     L.part = round_up(L.ml + rows_all * 8, 256);
     L.bytes = round_up(L.part + rows_all * d.d_latent * 4, 256);
     return L;

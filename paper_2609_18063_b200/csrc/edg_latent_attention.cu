@@ -4,8 +4,20 @@
 namespace edg {
 namespace {
 
-// Up to how many new rows a sequence is taken in the absorbed form when the caller leaves it open.
+// Up to how many new rows a sequence is taken in the absorbed form when the caller leaves it open.  Its work grows with them, the expanded
+// form's hardly does below 128 (32 heads of 128, 512 latent columns, microseconds absorbed / expanded):
+//     8 sequences of 2,000 positions:   16 rows  68 / 216    64: 220 / 217    128: 420 / 220
+//     one of 1,000:                     16 rows  31 /  39    64:  38 /  40    128:  60 /  40
+//     4 of 16,000:                      16 rows 135 / 826    64: 456 / 761    128: 925 / 776
 constexpr int kAbsorbedMost = 64;
+// Where some sequence has more, the others cost four launches in the absorbed form (20-40 us with little to do).  They are expanded along when
+// they are short: one prompt of 1,024 rows beside 4 sequences of 250 positions takes 64 us so and 83 in two forms, beside 16 of 250 125 and 97.
+// Their positions are known by their bound alone; 100 more for each stand for the CTAs of a sequence.
+constexpr int64_t kAlongPositions = 3500;
+bool expanded_along(const edg_latent_desc& d, int n_seqs, int max_new, int64_t total_len) {
+    const int64_t others = (total_len > max_new ? total_len - max_new : 0) + 100ll * (n_seqs - 1);
+    return n_seqs == 1 || others * (d.heads > 32 ? d.heads : 32) <= kAlongPositions * 32;
+}
 
 struct Forms {
     bool absorbed, expanded;
@@ -14,10 +26,13 @@ struct Forms {
 };
 Forms forms(const edg_latent_desc& d, int n_seqs, int T, int max_new, int64_t total_len) {
     Forms f;
-    f.most = d.form == EDG_LATENT_ABSORBED ? max_new : (d.form == EDG_LATENT_EXPANDED ? 0 : (max_new < kAbsorbedMost ? max_new : kAbsorbedMost));
+    if (d.form == EDG_LATENT_AUTO) f.most = max_new <= kAbsorbedMost ? max_new : (expanded_along(d, n_seqs, max_new, total_len) ? 0 : kAbsorbedMost);
+    else f.most = d.form == EDG_LATENT_ABSORBED ? max_new : 0;
     f.absorbed = f.most > 0;
     f.expanded = max_new > f.most;
-    f.first = round_up(f.absorbed ? absorbed_workspace(d, n_seqs, T, f.most) : kCtrlBytes, 256);
+    // (scratch for both where the form is open, so that what serves some bounds serves all smaller ones)
+    const int kept = d.form == EDG_LATENT_AUTO && max_new > kAbsorbedMost ? kAbsorbedMost : max_new;
+    f.first = round_up(d.form != EDG_LATENT_EXPANDED ? absorbed_workspace(d, n_seqs, T, kept) : kCtrlBytes, 256);
     f.bytes = f.first + (f.expanded ? expanded_workspace(d, n_seqs, T, total_len) : 0);
     return f;
 }
