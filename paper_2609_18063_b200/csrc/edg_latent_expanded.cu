@@ -6,13 +6,17 @@
 // 2 (d_n + d_r + d_v) operations a pair of rows against 2 (2 d_l + d_r) in the latent space, 3.4 times fewer at 128 / 64 / 128 / 512; the writing out costs
 // 2 d_l (d_n + d_v) a position and head, which some hundred new rows a sequence earn back.
 //
-// prompt_kernel: a CTA takes two tiles of 128 new rows of one head; while the softmax of one runs, the tensor cores work on the other.  S of
-// a tile (128 x 128) lies in tensor memory, a row to a lane: maximum and sum are a thread's own.  P goes back over S as bf16 and is the A
-// operand of P V from there.  O is rescaled only when a row's maximum has grown by more than 2^8.  Keys and values come by
-// TMA in chunks of 64 columns through one ring of eight (K of a tile, V of it, K of the next: the tile after that takes what S has read).
-// Positions behind a sequence's end are padded to 128; their values are written as zeros, their scores never looked at.
-#include <type_traits>
-
+// prompt_kernel: a CTA takes pairs of tiles of 128 new rows of a head; while the softmax of one runs, the tensor cores work on the other.  S of
+// a tile (128 x 128) lies in tensor memory, two threads to a row with half of its columns each.  P goes back over S as bf16 and is the A
+// operand of P V from there, the first half of it while the other is still being made.  O is rescaled only when a row's maximum has grown by
+// more than 2^8.  Keys and values come by TMA in chunks of 64 columns through one ring of eight (K of a tile, V of it, K of the next: the tile
+// after that takes what S has read).  Positions behind a sequence's end are padded to 128; their values are written as zeros, their scores
+// never looked at.
+//
+// 4,430 new rows of three sequences of 7,103 positions, 32 heads of 128 + 64 / 128, 512 latent columns: expand_kernel 62 us (62 GFLOP: 1.0
+// PFLOP/s; its limits are the weights, which every CTA reads from L2, and its two rounds of CTAs), prompt_kernel 182 us (185 GFLOP of rows that
+// see one another: 1.0 PFLOP/s).  A pair of tiles takes 3,900 clocks of which the tensor cores work 3,260; S of a tile, its softmax (2,050), P V
+// follow one another, since neither tensor memory has room for a third S nor shared memory for P.
 #include "edg_latent.cuh"
 #include "edg_umma.cuh"
 
@@ -23,6 +27,7 @@ struct ExpandedParams {
     const uint16_t* cache;
     uint16_t *K, *V, *Rp;       // [heads][rows][dn], [heads][rows][dv], [rows][64] (rotated part and zeros)
     int32_t *q_pre, *kv_pre;    // [n + 1] pairs of row tiles before a sequence; tiles of 128 positions before it
+    int32_t* next;              // the next pair of row tiles (of a head) to be taken
     void* y;
     int32_t* status;
     int heads, dn, dr, dv, dl, out_dtype;
@@ -50,8 +55,9 @@ __device__ __forceinline__ XSeq xsequence(const ExpandedParams& p, int i) {
 // prefix sums over the sequences, and the caller's bounds
 __global__ void __launch_bounds__(256) prompt_plan_kernel(const __grid_constant__ ExpandedParams p) {
     pdl_launch_dependents();
-    __shared__ int s_q[256], s_k[256];
-    __shared__ long long s_l[256];
+    if (threadIdx.x == 0) *p.next = 0;
+    __shared__ int s_q[8], s_k[8];
+    __shared__ long long s_l[8];
     const int tid = threadIdx.x, per = (p.s.n + 255) / 256, i0 = min(tid * per, p.s.n), i1 = min(i0 + per, p.s.n);
     int q = 0, k = 0;
     long long len = 0;
@@ -63,14 +69,21 @@ __global__ void __launch_bounds__(256) prompt_plan_kernel(const __grid_constant_
         len += x.len;
         ok = ok && p.s.cu[i + 1] >= p.s.cu[i] && x.fresh <= p.max_new && x.len >= p.s.lens[i];
     }
-    s_q[tid] = q;
-    s_k[tid] = k;
-    s_l[tid] = len;
+    const int lane = tid & 31, warp = tid >> 5, own_q = q, own_k = k;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {                                    // sums up to and with this lane's
+        const int a = __shfl_up_sync(0xFFFFFFFFu, q, d), b = __shfl_up_sync(0xFFFFFFFFu, k, d);
+        if (lane >= d) { q += a; k += b; }
+        len += __shfl_xor_sync(0xFFFFFFFFu, len, d);
+    }
+    if (lane == 31) { s_q[warp] = q; s_k[warp] = k; s_l[warp] = len; }
     __syncthreads();
-    q = k = 0;
+    q -= own_q;
+    k -= own_k;
     len = 0;
-    for (int j = 0; j < 256; ++j) {
-        if (j < tid) { q += s_q[j]; k += s_k[j]; }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if (j < warp) { q += s_q[j]; k += s_k[j]; }
         len += s_l[j];
     }
     if (!ok || len > p.total_len) latent_raise(p.status, EDG_E_RANGE);
@@ -147,44 +160,46 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
                     for (int c = 0; c < nc; ++c) tma_2d(sb + c * kChunk + b * br * 128, &c_map, c * 64, y, c_full);
                 __syncwarp();
             }
-            RingAt w;
-            bool moved = false;
-            for (int h = h0; h < h1; ++h)
-                for (int kv = 0; kv < 2; ++kv)
-                    for (int c = 0; c < nc; ++c) {
-                        role_wait(&w_empty[w.slot], w.phase ^ 1, p.status);
-                        if (w.slot >= 4 && !moved) { role_wait(a_full, 0, p.status); moved = true; }
-                        if (elected()) {
-                            const int n = kv == 0 ? p.dn : p.dv;
-                            tma_2d(sb + chunk_at(w.slot), kv == 0 ? &uk_map : &uv_map, c * 64, h * n, &w_full[w.slot]);
+            if (elected()) {
+                RingAt w;
+                bool moved = false;
+                for (int h = h0; h < h1; ++h)
+                    for (int kv = 0; kv < 2; ++kv) {
+                        const int n = kv == 0 ? p.dn : p.dv;
+                        const CUtensorMap* map = kv == 0 ? &uk_map : &uv_map;
+                        for (int c = 0; c < nc; ++c) {
+                            role_wait(&w_empty[w.slot], w.phase ^ 1, p.status);
+                            if (w.slot >= 4 && !moved) { role_wait(a_full, 0, p.status); moved = true; }
                             mbar_expect_tx(&w_full[w.slot], n * 128);
+                            tma_2d(sb + chunk_at(w.slot), map, c * 64, h * n, &w_full[w.slot]);
+                            w.next(kXRing);
                         }
-                        __syncwarp();
-                        w.next(kXRing);
                     }
+            }
+            __syncwarp();
         } else if (warp == 1) {
-            const uint32_t dw = desc_lo(sb);
-            RingAt w;
-            int j = 0;
-            role_wait(a_full, 0, p.status);
-            for (int h = h0; h < h1; ++h)
-                for (int kv = 0; kv < 2; ++kv, ++j) {
-                    const uint32_t id = idesc_bf16(128, kv == 0 ? p.dn : p.dv), d = tmem + (j & 1) * 128;
-                    role_wait(&d_empty[j & 1], ((uint32_t)(j >> 1) & 1) ^ 1, p.status);
-                    for (int c = 0; c < nc; ++c) {
-                        role_wait(&w_full[w.slot], w.phase, p.status);
-                        tc_fence_after();
-                        if (elected()) {
+            if (elected()) {                                             // (one thread: see the products of prompt_kernel)
+                const uint32_t dw = desc_lo(sb);
+                RingAt w;
+                int j = 0;
+                role_wait(a_full, 0, p.status);
+                for (int h = h0; h < h1; ++h)
+                    for (int kv = 0; kv < 2; ++kv, ++j) {
+                        const uint32_t id = idesc_bf16(128, kv == 0 ? p.dn : p.dv), d = tmem + (j & 1) * 128;
+                        role_wait(&d_empty[j & 1], ((uint32_t)(j >> 1) & 1) ^ 1, p.status);
+                        for (int c = 0; c < nc; ++c) {
+                            role_wait(&w_full[w.slot], w.phase, p.status);
+                            tc_fence_after();
                             const uint32_t a = tmem + 256 + c * 32, b = dw + (chunk_at(w.slot) >> 4);
 #pragma unroll
                             for (int k = 0; k < 4; ++k) umma_ts(d, a + k * 8, b + k * 2, id, c + k > 0);
                             umma_done(&w_empty[w.slot]);
-                            if (c == nc - 1) umma_done(&d_full[j & 1]);
+                            w.next(kXRing);
                         }
-                        __syncwarp();
-                        w.next(kXRing);
+                        umma_done(&d_full[j & 1]);
                     }
-                }
+            }
+            __syncwarp();
         } else if (warp >= 4) {
             const int wq = warp & 3, row = wq * 32 + lane;
             const uint32_t lanes = (uint32_t)(wq * 32) << 16;
@@ -261,10 +276,14 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
 
 // ---------------------------------------------------------------- attention
 
-constexpr int kPThreads = 640;              // warp 0 loads, warp 1 issues products, warps 4-11 and 12-19 are the softmax of a tile of rows each
+constexpr int kSms = 148;
+constexpr int kPThreads = 640;              // warp 0 takes work and loads, 1 issues products, 4-11 and 12-19 are the softmax of a tile of rows each
 constexpr int kPRing = 8;
-constexpr int kCubicOf = 8, kCubic = 2;     // of 8 weights, 2 are made on the multipliers
-constexpr uint32_t kPQ = 0, kPRingAt = 6 * kChunk, kPBars = kPRingAt + kPRing * kChunk, kPMax = kPBars + 256, kPBytes = kPMax + 2048;
+constexpr uint32_t kPQ = 0, kPRingAt = 6 * kChunk, kPBars = kPRingAt + kPRing * kChunk, kPItems = kPBars + 320, kPMax = kPItems + 64,
+                   kPBytes = kPMax + 2048;
+
+// Two tiles of 128 new rows of one head, and what they see.  h < 0: there is no more.
+struct alignas(16) Item { int h, kv0, pos0, token, rows, n[2], unused; };
 
 __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_constant__ ExpandedParams p, const __grid_constant__ CUtensorMap qn_map,
                                                               const __grid_constant__ CUtensorMap qr_map, const __grid_constant__ CUtensorMap k_map,
@@ -276,8 +295,13 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
     uint64_t* q_full = kv_full + kPRing;                                      // [2]
     uint64_t* s_full = q_full + 2;                                       // [2]
     uint64_t* p_full = s_full + 2;                                       // [2]
-    uint64_t* o_done = p_full + 2;                                       // [2]
-    uint32_t* s_tmem = reinterpret_cast<uint32_t*>(o_done + 2);
+    uint64_t* p_half = p_full + 2;                                       // [2] the first 32 columns of both halves of a tile's P
+    uint64_t* o_done = p_half + 2;                                       // [2]
+    uint64_t* q_empty = o_done + 2;                                      // [2] the last S of a tile of rows is there
+    uint64_t* item_full = q_empty + 2;                                   // [2]
+    uint64_t* item_empty = item_full + 2;                                // [2]
+    uint32_t* s_tmem = reinterpret_cast<uint32_t*>(item_empty + 2);
+    Item* s_item = reinterpret_cast<Item*>(smem + kPItems);              // [2]
     float* s_max = reinterpret_cast<float*>(smem + kPMax);               // [tile][half of the columns][row]
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if ((sb & 1023) != 0) {                                              // (the swizzle counts on it)
@@ -287,8 +311,14 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
     if (tid == 0) {
         for (int i = 0; i < kPRing; ++i) mbar_init(&kv_empty[i], 1);
         for (int i = 0; i < kPRing; ++i) mbar_init(&kv_full[i], 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&q_full[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 8); mbar_init(&o_done[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&q_full[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 8); mbar_init(&p_half[i], 8); mbar_init(&o_done[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&q_empty[i], 1); mbar_init(&item_full[i], 1); mbar_init(&item_empty[i], 17); s_item[i].h = -1; }
         fence_barrier_init();
+        prefetch_map(&qn_map);
+        prefetch_map(&qr_map);
+        prefetch_map(&k_map);
+        prefetch_map(&r_map);
+        prefetch_map(&v_map);
     }
     if (warp == 1) tmem_alloc(s_tmem, 512);
     pdl_wait_prior_grid();
@@ -296,21 +326,18 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *s_tmem;
-    const int h = blockIdx.x % p.heads, pairs = p.q_pre[p.s.n];
-    const int pair = pairs - 1 - (int)(blockIdx.x / p.heads);                        // (the last rows of a sequence see the most: they go first)
-    const int seq = pair >= 0 ? find_sequence(p.q_pre, p.s.n, pair, lane) : p.s.n;
-    if (seq < p.s.n) {
-        const XSeq q = xsequence(p, seq);
-        const int r0 = (pair - p.q_pre[seq]) * 256, kv0 = p.kv_pre[seq] * 128;
-        const bool fits = kv0 + q.tiles * 128 <= p.rows;
-        const int pos0 = q.len - q.fresh + r0;                           // position of the pair's first row
-        int n[2];                                                        // tiles of 128 positions that a tile of rows sees something of
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int last = min(r0 + i * 128 + 127, q.fresh - 1);      // its last row
-            n[i] = fits && r0 + i * 128 < q.fresh ? max((q.len - q.fresh + last + 128) >> 7, 0) : 0;
-        }
-        const int nt = max(n[0], n[1]);
+    // A CTA takes pairs of tiles one after another: the next one's queries and keys are loaded, and its first tile begun, while the second tile
+    // of this one is finished (a CTA a pair stood for 5,000 clocks before its first S and 5,000 after its last, of some 75,000).
+    RingAt it;
+    auto take_item = [&](Item& x) {
+        role_wait(&item_full[it.slot], it.phase, p.status);
+        x = s_item[it.slot];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&item_empty[it.slot]);
+        it.next(2);
+        return x.h >= 0;
+    };
+    {
         const int nkc = (p.dn + 63) / 64, nvc = (p.dv + 63) / 64;        // chunks of keys (and one of rotated parts), of values
         if (warp >= 4) {
             // ========================================= softmax: two threads to a row, 64 columns each (one thread's 128 took 2000 clocks from S to P,
@@ -318,13 +345,16 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
             const int i = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, wq = warp & 3, row = i * 128 + wq * 32 + lane;
             const uint32_t st = tmem + ((uint32_t)(wq * 32) << 16) + i * 128, ot = st + 256;
             const float k2 = p.scale * 1.4426950408889634f;
-            const int pos = pos0 + row;                                  // positions 0 .. pos are seen
             float* my_max = s_max + (i * 2 + half) * 128 + wq * 32 + lane;
             const float* their_max = s_max + (i * 2 + 1 - half) * 128 + wq * 32 + lane;
+            uint32_t done = 0;                                           // tiles, of all items
+            Item x;
+            while (take_item(x)) {
+            const int pos = x.pos0 + row, mine = i == 0 ? x.n[0] : x.n[1];        // positions 0 .. pos are seen
+            uint16_t* const out = row < x.rows ? static_cast<uint16_t*>(p.y) + ((size_t)(x.token + row) * p.heads + x.h) * p.dv : nullptr;
             float m = -INFINITY, l = 0.f;                                // (l: of this thread's columns)
-            const int mine = i == 0 ? n[0] : n[1];
-            for (int t = 0; t < mine; ++t) {
-                role_wait(&s_full[i], (uint32_t)t & 1, p.status);
+            for (int t = 0; t < mine; ++t, ++done) {
+                role_wait(&s_full[i], done & 1, p.status);
                 tc_fence_after();
                 const int seen = pos + 1 - t * 128 - half * 64;          // of these columns
                 const bool part = __any_sync(0xFFFFFFFFu, seen < 64);
@@ -357,7 +387,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                 if (__any_sync(0xFFFFFFFFu, grown)) {                    // (the same rows in both halves; each takes every second 16 columns of O)
                     const float alpha = grown ? exp2_approx(m - mt) : 1.f;
                     if (grown) { m = mt; l *= alpha; }
-                    role_wait(&o_done[i], (uint32_t)(t - 1) & 1, p.status);
+                    role_wait(&o_done[i], (done - 1) & 1, p.status);
                     tc_fence_after();
                     for (int c = half * 16; c < p.dv; c += 32) {
                         uint32_t o[16];
@@ -370,25 +400,24 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                 }
                 const float mm = m == -INFINITY ? 0.f : -m;
                 float2 sum = make_float2(0.f, 0.f);
-                // (masked scores are -infinity: ex2 makes zeros of them, the cubic would not)
-                auto weights = [&](auto cubic) {
 #pragma unroll
-                    for (int c = 0; c < 64; c += 32) {
-                        uint32_t o[16];
+                for (int c = 0; c < 64; c += 32) {
+                    uint32_t o[16];
 #pragma unroll
-                        for (int j = 0; j < 32; j += 2) {
-                            const float a = fmaf(__uint_as_float(v[c + j]), k2, mm), b = fmaf(__uint_as_float(v[c + j + 1]), k2, mm);
-                            const bool multiply = decltype(cubic)::value && j % kCubicOf < kCubic;
-                            const float x = multiply ? exp2_cubic(a) : exp2_approx(a), y = multiply ? exp2_cubic(b) : exp2_approx(b);
-                            sum.x += x;
-                            sum.y += y;
-                            o[j / 2] = bf16_pair(x, y);
-                        }
-                        tmem_st(st + half * 32 + c / 2, o);              // (over the scores of the first half, which all have read: the barrier above)
+                    for (int j = 0; j < 32; j += 2) {
+                        const float x = exp2_approx(fmaf(__uint_as_float(v[c + j]), k2, mm)), y = exp2_approx(fmaf(__uint_as_float(v[c + j + 1]), k2, mm));
+                        sum.x += x;
+                        sum.y += y;
+                        o[j / 2] = bf16_pair(x, y);
                     }
-                };
-                if (part) weights(std::false_type());
-                else weights(std::true_type());
+                    tmem_st(st + half * 32 + c / 2, o);                  // (over the scores of the first half, which all have read: the barrier above)
+                    if (c == 0) {                                        // (half of P V can begin)
+                        tmem_st_wait();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&p_half[i]);
+                    }
+                }
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
@@ -396,52 +425,56 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                 l += sum.x + sum.y;
             }
             // ---- out
-            if (mine > 0) {
-                role_wait(&o_done[i], (uint32_t)(mine - 1) & 1, p.status);
-                tc_fence_after();
+            // (straight from the registers, a sector at a time: by way of the queries' place, for whole lines, the next queries came 6,000 clocks later)
+            if (mine == 0) {                                             // rows that see nothing, or none
+                if (out != nullptr)
+                    for (int c = half * 16; c < p.dv; c += 32) {
+                        *reinterpret_cast<uint4*>(out + c) = make_uint4(0, 0, 0, 0);
+                        *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(0, 0, 0, 0);
+                    }
+                continue;
             }
             *my_max = l;
             barrier_sync(1 + i, 256);
             l += *their_max;
-            // (by way of this tile's queries, which nothing reads any more; the two halves take every second 16 columns, then every second row)
+            barrier_sync(1 + i, 256);                                    // (the next item's maxima go there)
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            uint8_t* stage = smem + kPQ + i * 3 * kChunk + wq * 8192;
-            for (int c = half * 16; c < p.dv; c += 32) {
+            role_wait(&o_done[i], (done - 1) & 1, p.status);
+            tc_fence_after();
+            for (int c = half * 16; c < p.dv; c += 32) {                 // (the two halves take every second 16 columns)
                 uint32_t v[16], o[8];
-                if (mine > 0) tmem_ld(ot + c, v);
-                else
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] = 0u;
+                tmem_ld(ot + c, v);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float a = l == 0.f ? 0.f : __uint_as_float(v[2 * j]) * inv, b = l == 0.f ? 0.f : __uint_as_float(v[2 * j + 1]) * inv;
                     if (p.out_dtype == EDG_F16) {
-                        const __half2 x = __floats2half2_rn(a, b);
-                        o[j] = *reinterpret_cast<const uint32_t*>(&x);
+                        const __half2 y = __floats2half2_rn(a, b);
+                        o[j] = *reinterpret_cast<const uint32_t*>(&y);
                     } else o[j] = bf16_pair(a, b);
                 }
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    *reinterpret_cast<uint4*>(stage + lane * 256 + (((c / 8 + x) ^ (lane & 7)) * 16)) = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+                if (out != nullptr) {
+                    *reinterpret_cast<uint4*>(out + c) = make_uint4(o[0], o[1], o[2], o[3]);
+                    *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+                }
+                __syncwarp();
             }
-            barrier_sync(1 + i, 256);
-            const int pieces = p.dv / 8, first = r0 + i * 128 + wq * 32, rows = fits ? min(q.fresh - first, 32) : 0;
-            for (int x = half * 32 + lane; x < rows * pieces; x += 64) {
-                const int rr = x / pieces, c = x - rr * pieces;
-                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y) + ((size_t)(q.a + first + rr) * p.heads + h) * p.dv + c * 8) =
-                    *reinterpret_cast<const uint4*>(stage + rr * 256 + ((c ^ (rr & 7)) * 16));
+            tc_fence_before();
             }
         } else {
             if (warp == 0) {
             // ========================================= loads
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (n[i] > 0 && elected()) {
+            uint32_t begun[2] = {0, 0};
+            Item x = {};
+            auto queries = [&](int i) {
+                if (x.n[i] == 0) return;
+                role_wait(&q_empty[i], (begun[i]++ & 1) ^ 1, p.status);
+                if (elected()) {
                     mbar_expect_tx(&q_full[i], (nkc + 1) * kChunk);
-                    for (int c = 0; c < nkc; ++c) tma_3d(sb + kPQ + (i * 3 + c) * kChunk, &qn_map, c * 64, h, q.a + r0 + i * 128, &q_full[i]);
-                    tma_3d(sb + kPQ + (i * 3 + nkc) * kChunk, &qr_map, 0, h, q.a + r0 + i * 128, &q_full[i]);
+                    for (int c = 0; c < nkc; ++c) tma_3d(sb + kPQ + (i * 3 + c) * kChunk, &qn_map, c * 64, x.h, x.token + i * 128, &q_full[i]);
+                    tma_3d(sb + kPQ + (i * 3 + nkc) * kChunk, &qr_map, 0, x.h, x.token + i * 128, &q_full[i]);
                 }
-            __syncwarp();
+                __syncwarp();
+            };
             // Groups (the keys of a tile, its values, the next keys ...) take the ring's chunks in turn and are read in that order: a group waits
             // until those before it have left it room.
             RingAt f, old;
@@ -456,36 +489,81 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                     old.next(kPRing);
                 }
             };
+            // ---- work: the last pairs of a sequence see the most, they go first.  (The next one is taken when all of this one's loads are on their
+            // way, not before: taken a whole pair ahead, the last CTA had 82 of 67 tiles on average.)
+            const int total = p.q_pre[p.s.n] * p.heads;
+            auto next_item = [&]() {
+                int w = 0;
+                if (lane == 0) w = atomicAdd(p.next, 1);
+                w = __shfl_sync(0xFFFFFFFFu, w, 0);
+                x.h = -1;
+                if (w >= 0 && w < total) {
+                    const int pair = total / p.heads - 1 - w / p.heads, seq = min(find_sequence(p.q_pre, p.s.n, pair, lane), p.s.n - 1);
+                    const XSeq q = xsequence(p, seq);
+                    const int r0 = (pair - p.q_pre[seq]) * 256;
+                    x.h = w % p.heads;
+                    x.kv0 = p.kv_pre[seq] * 128;
+                    const bool fits = x.kv0 + q.tiles * 128 <= p.rows;
+                    x.pos0 = q.len - q.fresh + r0;                       // position of the pair's first row
+                    x.token = q.a + r0;
+                    x.rows = fits ? q.fresh - r0 : 0;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {                        // tiles of 128 positions that a tile of rows sees something of
+                        const int last = min(r0 + i * 128 + 127, q.fresh - 1);      // its last row
+                        x.n[i] = fits && r0 + i * 128 < q.fresh ? max((q.len - q.fresh + last + 128) >> 7, 0) : 0;
+                    }
+                }
+                role_wait(&item_empty[it.slot], it.phase ^ 1, p.status);
+                if (lane == 0) {
+                    s_item[it.slot] = x;
+                    mbar_arrive(&item_full[it.slot]);
+                }
+                __syncwarp();
+                it.next(2);
+                return x.h >= 0;
+            };
+            while (next_item()) {
+            const int nt = max(x.n[0], x.n[1]);
+            queries(0);
             for (int t = 0; t < nt; ++t) {
-                const int row = kv0 + t * 128;
+                const int row = x.kv0 + t * 128;
                 room(nkc + 1);
                 if (elected()) {
                     mbar_expect_tx(&kv_full[f.slot], (nkc + 1) * kChunk);
-                    for (int c = 0; c < nkc; ++c) tma_3d(sb + kPRingAt + ((at + c) & (kPRing - 1)) * kChunk, &k_map, c * 64, row, h, &kv_full[f.slot]);
+                    for (int c = 0; c < nkc; ++c) tma_3d(sb + kPRingAt + ((at + c) & (kPRing - 1)) * kChunk, &k_map, c * 64, row, x.h, &kv_full[f.slot]);
                     tma_2d(sb + kPRingAt + ((at + nkc) & (kPRing - 1)) * kChunk, &r_map, 0, row, &kv_full[f.slot]);
                 }
                 __syncwarp();
                 at = (at + nkc + 1) & (kPRing - 1);
                 f.next(kPRing);
+                if (t == 0) queries(1);                         // (free later than the first tile's, and needed later)
                 room(nvc);
                 if (elected()) {
                     mbar_expect_tx(&kv_full[f.slot], nvc * kChunk);
-                    for (int c = 0; c < nvc; ++c) tma_3d(sb + kPRingAt + ((at + c) & (kPRing - 1)) * kChunk, &v_map, c * 64, row, h, &kv_full[f.slot]);
+                    for (int c = 0; c < nvc; ++c) tma_3d(sb + kPRingAt + ((at + c) & (kPRing - 1)) * kChunk, &v_map, c * 64, row, x.h, &kv_full[f.slot]);
                 }
                 __syncwarp();
                 at = (at + nvc) & (kPRing - 1);
                 f.next(kPRing);
             }
+            }
         } else if (warp == 1) {
-            // ========================================= products.  For each tile of rows O += P V of a tile of positions, then S of the next
-            const uint32_t id_s = idesc_bf16(128, 128), id_o = idesc_bf16(128, p.dv, false, true);
-            const uint32_t dq = desc_lo(sb + kPQ), dk = desc_lo(sb + kPRingAt), dv = desc_lo(sb + kPRingAt, kChunk);
-            const int rks = p.dr / 16;
-            RingAt f;                                                    // the next group (keys or values) to wait for
-            int at = 0;                                                  // ring place of the next group
-            auto take = [&](int chunks) { const int a = at; at = (at + chunks) & (kPRing - 1); return a; };
-            auto scores = [&](int i, int k) {
-                if (elected()) {
+            // ========================================= products, by one thread: for each tile of rows O += P V of a tile of positions, then S of the
+            // next.  (What it does between two products is time in which the tensor cores wait: they hold two or three products of 65 clocks.)
+            if (elected()) {
+                const uint32_t id_s = idesc_bf16(128, 128), id_o = idesc_bf16(128, p.dv, false, true);
+                const uint32_t dq = desc_lo(sb + kPQ), dk = desc_lo(sb + kPRingAt), dv = desc_lo(sb + kPRingAt, kChunk);
+                const int rks = p.dr / 16;
+                RingAt f;                                                // the next group (keys or values) to wait for
+                int at = 0, read = 0;                                    // ring place of the next group; groups that have been read
+                uint32_t tiles[2] = {0, 0}, begun[2] = {0, 0};           // tiles of positions, tiles of rows with any
+                auto take = [&](int chunks) { const int a = at; at = (at + chunks) & (kPRing - 1); return a; };
+                auto loaded = [&](RingAt g) {
+                    role_wait(&kv_full[g.slot], g.phase, p.status);
+                    tc_fence_after();
+                };
+                auto release = [&]() { umma_done(&kv_empty[read++ & (kPRing - 1)]); };
+                auto scores = [&](int i, int k, bool last) {
                     const uint32_t st = tmem + i * 128;
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
@@ -499,79 +577,82 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                     for (int s = 0; s < 4; ++s)
                         if (s < rks) umma_ss(st, a + s * 2, b + s * 2, id_s, true);
                     umma_done(&s_full[i]);
-                }
-                __syncwarp();
-            };
-            int read = 0;                                                // groups
-            auto release = [&]() {
-                if (elected()) umma_done(&kv_empty[read & (kPRing - 1)]);
-                __syncwarp();
-                ++read;
-            };
-            int k = 0;
-            if (nt > 0) {
-                k = take(nkc + 1);
-                role_wait(&kv_full[f.slot], f.phase, p.status);
-                f.next(kPRing);
+                    if (last) umma_done(&q_empty[i]);
+                };
+                while (true) {
+                    role_wait(&item_full[it.slot], it.phase, p.status);
+                    const int n[2] = {s_item[it.slot].n[0], s_item[it.slot].n[1]};
+                    const bool end = s_item[it.slot].h < 0;
+                    mbar_arrive(&item_empty[it.slot]);
+                    it.next(2);
+                    if (end) break;
+                    const int nt = max(n[0], n[1]);
+                    int k = 0;
+                    if (nt > 0) {
+                        k = take(nkc + 1);
+                        loaded(f);
+                        f.next(kPRing);
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (n[i] > 0) {
-                        role_wait(&q_full[i], 0, p.status);
-                        tc_fence_after();
-                        scores(i, k);
-                    }
-                release();
-            }
-            for (int t = 0; t < nt; ++t) {
-                const int v = take(nvc);
-                const RingAt fv = f;                                     // the values, and the next keys
-                f.next(kPRing);
-                const bool more = t + 1 < nt;
-                const RingAt fk = f;
-                if (more) { k = take(nkc + 1); f.next(kPRing); }
-                const bool whole = nvc == 1 || v + 1 < kPRing;           // (values that go round the ring's end: a chunk at a time)
-                const uint32_t b = dv + ((v * kChunk) >> 4);
-                bool seen_v = false, seen_k = false;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t o = tmem + 256 + i * 128, pt = tmem + i * 128;
-                    if (t < n[i]) {
-                        if (!seen_v) role_wait(&kv_full[fv.slot], fv.phase, p.status);
-                        seen_v = true;
-                        if (t + 1 < n[i] && !seen_k) {
-                            role_wait(&kv_full[fk.slot], fk.phase, p.status);
-                            seen_k = true;
-                        }
-                        role_wait(&p_full[i], (uint32_t)t & 1, p.status);
-                        tc_fence_after();
-                        if (elected()) {
-                            if (whole) {
-#pragma unroll
-                                for (int s = 0; s < 8; ++s) umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id_o, t + s > 0);
-                            } else {
-                                const uint32_t id0 = idesc_bf16(128, 64, false, true), id1 = idesc_bf16(128, p.dv - 64, false, true);
-#pragma unroll
-                                for (int s = 0; s < 8; ++s) {
-                                    umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id0, t + s > 0);
-                                    umma_ts(o + 64, pt + s * 8, dv + ((s * 2048) >> 4), id1, t + s > 0);
-                                }
+                        for (int i = 0; i < 2; ++i)
+                            if (n[i] > 0) {
+                                role_wait(&q_full[i], begun[i]++ & 1, p.status);
+                                tc_fence_after();
+                                scores(i, k, n[i] == 1);
                             }
-                            umma_done(&o_done[i]);
-                        }
-                        __syncwarp();
+                        release();
                     }
-                    if (i == 1) release();                               // (the values)
-                    if (t + 1 < n[i]) {
-                        if (!seen_k) {                                   // (a tile of rows that begins here)
-                            role_wait(&kv_full[fk.slot], fk.phase, p.status);
-                            tc_fence_after();
-                            seen_k = true;
+                    for (int t = 0; t < nt; ++t) {
+                        const int v = take(nvc);
+                        const RingAt fv = f;                             // the values, and the next keys
+                        f.next(kPRing);
+                        const bool more = t + 1 < nt;
+                        const RingAt fk = f;
+                        if (more) { k = take(nkc + 1); f.next(kPRing); }
+                        const bool whole = nvc == 1 || v + 1 < kPRing;   // (values that go round the ring's end: a chunk at a time)
+                        const uint32_t b = dv + ((v * kChunk) >> 4);
+                        bool seen_v = false, seen_k = false;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t o = tmem + 256 + i * 128, pt = tmem + i * 128;
+                            if (t < n[i]) {
+                                if (!seen_v) loaded(fv);
+                                seen_v = true;
+                                role_wait(&p_half[i], tiles[i] & 1, p.status);
+                                tc_fence_after();
+                                if (whole) {                             // (16 positions each: 0-31, 64-95, then the others)
+#pragma unroll
+                                    for (int x = 0; x < 8; ++x) {
+                                        const int s = (x & 1) | (x & 2) << 1 | (x & 4) >> 1;
+                                        if (x == 4) {
+                                            role_wait(&p_full[i], tiles[i]++ & 1, p.status);
+                                            tc_fence_after();
+                                        }
+                                        umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id_o, t + x > 0);
+                                    }
+                                } else {
+                                    role_wait(&p_full[i], tiles[i]++ & 1, p.status);
+                                    tc_fence_after();
+                                    const uint32_t id0 = idesc_bf16(128, 64, false, true), id1 = idesc_bf16(128, p.dv - 64, false, true);
+#pragma unroll
+                                    for (int s = 0; s < 8; ++s) {
+                                        umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id0, t + s > 0);
+                                        umma_ts(o + 64, pt + s * 8, dv + ((s * 2048) >> 4), id1, t + s > 0);
+                                    }
+                                }
+                                umma_done(&o_done[i]);
+                            }
+                            if (i == 1) release();                       // (the values)
+                            if (t + 1 < n[i]) {
+                                if (!seen_k) loaded(fk);
+                                seen_k = true;
+                                scores(i, k, t + 2 == n[i]);
+                            }
                         }
-                        scores(i, k);
+                        if (more) release();
                     }
                 }
-                if (more) release();
             }
+            __syncwarp();
             }
         }
     }
@@ -581,7 +662,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
     if (warp == 1) tmem_free(tmem, 512);
 }
 
-struct ExpandedLayout { int rows; size_t q_pre, kv_pre, K, V, Rp, bytes; };
+struct ExpandedLayout { int rows; size_t q_pre, kv_pre, next, K, V, Rp, bytes; };
 
 ExpandedLayout expanded_layout(const edg_latent_desc& d, int n_seqs, int T, int64_t total_len) {
     ExpandedLayout L;
@@ -589,7 +670,8 @@ ExpandedLayout expanded_layout(const edg_latent_desc& d, int n_seqs, int T, int6
     L.rows = (int)(rows < 0x7FFFFF00 ? rows : 0x7FFFFF00);
     L.q_pre = 0;
     L.kv_pre = round_up(((size_t)n_seqs + 1) * 4, 256);
-    L.Rp = 2 * L.kv_pre;
+    L.next = 2 * L.kv_pre;
+    L.Rp = L.next + 256;
     L.K = L.Rp + (size_t)rows * 128;
     L.V = round_up(L.K + (size_t)rows * d.heads * d.d_nope * 2, 256);
     L.bytes = round_up(L.V + (size_t)rows * d.heads * d.d_v * 2, 256);
@@ -612,6 +694,7 @@ int32_t run_expanded(const edg_latent_desc& d, const LatentSeqs& s, int max_new,
     p.Rp = reinterpret_cast<uint16_t*>(ws + L.Rp);
     p.q_pre = reinterpret_cast<int32_t*>(ws + L.q_pre);
     p.kv_pre = reinterpret_cast<int32_t*>(ws + L.kv_pre);
+    p.next = reinterpret_cast<int32_t*>(ws + L.next);
     p.y = y;
     p.status = status;
     p.heads = d.heads;
@@ -679,8 +762,8 @@ int32_t run_expanded(const edg_latent_desc& d, const LatentSeqs& s, int max_new,
     prompt_plan_kernel<<<1, 256, 0, st>>>(p);
     EDG_CUDA_TRY(cudaGetLastError());
     EDG_CUDA_TRY(launch_pdl(expand_kernel, dim3((unsigned)tiles, p.splits), kXThreads, kXBytes, st, p, c_map, uk_map, uv_map));
-    const int with = s.n < s.T ? s.n : s.T;
-    EDG_CUDA_TRY(launch_pdl(prompt_kernel, dim3(d.heads * (s.T / 256 + with)), kPThreads, kPBytes, st, p, qn_map, qr_map, k_map, r_map, v_map));
+    const int64_t pairs = (int64_t)d.heads * (s.T / 256 + (s.n < s.T ? s.n : s.T));       // at most
+    EDG_CUDA_TRY(launch_pdl(prompt_kernel, dim3((unsigned)(pairs < kSms ? pairs : kSms)), kPThreads, kPBytes, st, p, qn_map, qr_map, k_map, r_map, v_map));
     return EDG_OK;
 }
 
