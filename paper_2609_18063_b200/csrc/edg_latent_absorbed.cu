@@ -385,29 +385,29 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
     } else if (warp == 1) {
         // ============================================= S of every tile, in two halves as they arrive.  (O is another warp's: what queues up
         // behind a product covers two or three of them, a wait costs as much, and each warp's products cover the other's waits.)
-        const uint32_t id_s = idesc_bf16(64, 64);
-        const uint32_t dq = desc_lo(sb + P::q), dk0 = desc_lo(sb + P::unit), dr0 = desc_lo(sb + P::rope);
-        const int rks = p.dr / 16;
-        RingAt ks, kr, f;
-        int n = 0;                                                       // tiles issued
-        uint32_t q_phase = 0;
-        while (w.next(p, g, r)) {
-            role_wait(q_full, q_phase, p.status);
-            q_phase ^= 1;
-            for (int t = w.t0; t < w.t1; ++t, ++n) {
-                const int buf = n & 1;
-                role_wait(&s_empty[buf], ((uint32_t)(n >> 1) & 1) ^ 1, p.status);
-                role_wait(&t_full[2 * f.slot], f.phase, p.status);
-                uint32_t at[4];
+        if (elected()) {
+            const uint32_t id_s = idesc_bf16(64, 64);
+            const uint32_t dq = desc_lo(sb + P::q), dk0 = desc_lo(sb + P::unit), dr0 = desc_lo(sb + P::rope);
+            const int rks = p.dr / 16;
+            RingAt ks, kr, f;
+            int n = 0;                                                       // tiles issued
+            uint32_t q_phase = 0;
+            while (w.next(p, g, r)) {
+                role_wait(q_full, q_phase, p.status);
+                q_phase ^= 1;
+                for (int t = w.t0; t < w.t1; ++t, ++n) {
+                    const int buf = n & 1;
+                    role_wait(&s_empty[buf], ((uint32_t)(n >> 1) & 1) ^ 1, p.status);
+                    role_wait(&t_full[2 * f.slot], f.phase, p.status);
+                    uint32_t at[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (u < NU) {
-                        at[u] = dk0 + ((ks.slot * kUnit) >> 4);
-                        ks.next(P::NV);
-                    }
-                tc_fence_after();
-                const uint32_t d = tmem + buf * 64, dr = dr0 + ((kr.slot * kRope) >> 4);
-                if (elected()) {
+                    for (int u = 0; u < 4; ++u)
+                        if (u < NU) {
+                            at[u] = dk0 + ((ks.slot * kUnit) >> 4);
+                            ks.next(P::NV);
+                        }
+                    tc_fence_after();
+                    const uint32_t d = tmem + buf * 64, dr = dr0 + ((kr.slot * kRope) >> 4);
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         if (k < rks) umma_ss(d, dq + ((NU * 2 * R * 128 + k * 32) >> 4), dr + ((k * 32) >> 4), id_s, k > 0);
@@ -422,12 +422,9 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                         umma_done(&s_full[buf]);
                         if (t == w.t1 - 1) umma_done(q_empty);
                     }
-                }
-                __syncwarp();
-                if (n1 < NU) {
-                    role_wait(&t_full[2 * f.slot + 1], f.phase, p.status);
-                    tc_fence_after();
-                    if (elected()) {
+                    if (n1 < NU) {
+                        role_wait(&t_full[2 * f.slot + 1], f.phase, p.status);
+                        tc_fence_after();
 #pragma unroll
                         for (int u = 1; u < 4; ++u)
                             if (u >= n1 && u < NU)
@@ -437,31 +434,31 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                         umma_done(&s_full[buf]);
                         if (t == w.t1 - 1) umma_done(q_empty);
                     }
-                    __syncwarp();
+                    f.next(kFull);
+                    kr.next(P::NR);
                 }
-                f.next(kFull);
-                kr.next(P::NR);
             }
         }
+        __syncwarp();
     } else if (warp == 2) {
         // ============================================= O += C^T P^T of every tile
-        const uint32_t id_o = idesc_bf16(128, R, true, false);
-        const uint32_t dp = desc_lo(sb + P::p), dv0 = desc_lo(sb + P::unit, kRope), o0 = tmem + 128;
-        RingAt vs;
-        int n = 0;
-        uint32_t o_phase = 1;
-        while (w.next(p, g, r)) {
-            role_wait(o_empty, o_phase, p.status);
-            o_phase ^= 1;
-            for (int t = w.t0; t < w.t1; ++t, ++n) {
-                role_wait(p_full, (uint32_t)n & 1, p.status);            // (whose writers have seen S: the units are there)
-                tc_fence_after();
-                RingAt at[4];
+        if (elected()) {
+            const uint32_t id_o = idesc_bf16(128, R, true, false);
+            const uint32_t dp = desc_lo(sb + P::p), dv0 = desc_lo(sb + P::unit, kRope), o0 = tmem + 128;
+            RingAt vs;
+            int n = 0;
+            uint32_t o_phase = 1;
+            while (w.next(p, g, r)) {
+                role_wait(o_empty, o_phase, p.status);
+                o_phase ^= 1;
+                for (int t = w.t0; t < w.t1; ++t, ++n) {
+                    role_wait(p_full, (uint32_t)n & 1, p.status);            // (whose writers have seen S: the units are there)
+                    tc_fence_after();
+                    RingAt at[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (u < NU) { at[u] = vs; vs.next(P::NV); }
-                const bool more = t > w.t0;
-                if (elected()) {
+                    for (int u = 0; u < 4; ++u)
+                        if (u < NU) { at[u] = vs; vs.next(P::NV); }
+                    const bool more = t > w.t0;
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
                         if (u < NU) {
@@ -472,9 +469,9 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
                         }
                     umma_done(pv_done);
                 }
-                __syncwarp();
             }
         }
+        __syncwarp();
     } else if (warp >= 4) {
         // ============================================= softmax, rescaling, epilogue
         // A product of M = 64 leaves its rows in 16 lanes of every 32; a load of that shape gives a lane two rows (gq, gq + 8 of the warp's
