@@ -6,14 +6,14 @@ namespace {
 
 // Up to how many new rows a sequence is taken in the absorbed form when the caller leaves it open.  Its work grows with them, the expanded
 // form's hardly does below 128 (32 heads of 128, 512 latent columns, microseconds absorbed / expanded):
-//     8 sequences of 2,000 positions:   16 rows  68 / 216    64: 220 / 217    128: 420 / 220
-//     one of 1,000:                     16 rows  31 /  39    64:  38 /  40    128:  60 /  40
-//     4 of 16,000:                      16 rows 135 / 826    64: 456 / 761    128: 925 / 776
+//     8 sequences of 2,000 positions:   16 rows  68 / 186    64: 223 / 187    128: 428 / 190
+//     one of 1,000:                     16 rows  31 /  34    64:  39 /  34    128:  60 /  35
+//     4 of 16,000:                      16 rows 142 / 711    64: 497 / 716    128: 948 / 694
 constexpr int kAbsorbedMost = 64;
 // Where some sequence has more, the others cost four launches in the absorbed form (20-40 us with little to do).  They are expanded along when
-// they are short: one prompt of 1,024 rows beside 4 sequences of 250 positions takes 64 us so and 83 in two forms, beside 16 of 250 125 and 97.
+// they are short: a prompt of 1,024 rows beside 8 sequences of 500 positions takes 83 us so and 100 in two forms, beside 4 of 4,000 197 and 179.
 // Their positions are known by their bound alone; 100 more for each stand for the CTAs of a sequence.
-constexpr int64_t kAlongPositions = 3500;
+constexpr int64_t kAlongPositions = 5000;
 bool expanded_along(const edg_latent_desc& d, int n_seqs, int max_new, int64_t total_len) {
     const int64_t others = (total_len > max_new ? total_len - max_new : 0) + 100ll * (n_seqs - 1);
     return n_seqs == 1 || others * (d.heads > 32 ? d.heads : 32) <= kAlongPositions * 32;

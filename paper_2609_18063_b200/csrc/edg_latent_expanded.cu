@@ -480,14 +480,15 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
             RingAt f, old;
             int at = 0, held = 0;                                        // place of the next chunk; chunks that have not been read
             bool old_keys = true;
+            auto room_left = [&]() {
+                role_wait(&kv_empty[old.slot], old.phase, p.status);
+                held -= old_keys ? nkc + 1 : nvc;
+                old_keys = !old_keys;
+                old.next(kPRing);
+            };
             auto room = [&](int chunks) {
                 held += chunks;
-                while (held > kPRing) {
-                    role_wait(&kv_empty[old.slot], old.phase, p.status);
-                    held -= old_keys ? nkc + 1 : nvc;
-                    old_keys = !old_keys;
-                    old.next(kPRing);
-                }
+                while (held > kPRing) room_left();
             };
             // ---- work: the last pairs of a sequence see the most, they go first.  (The next one is taken when all of this one's loads are on their
             // way, not before: taken a whole pair ahead, the last CTA had 82 of 67 tiles on average.)
@@ -547,6 +548,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                 f.next(kPRing);
             }
             }
+            while (held > 0) room_left();                                // (no arrival may come after the block's end)
         } else if (warp == 1) {
             // ========================================= products, by one thread: for each tile of rows O += P V of a tile of positions, then S of the
             // next.  (What it does between two products is time in which the tensor cores wait: they hold two or three products of 65 clocks.)

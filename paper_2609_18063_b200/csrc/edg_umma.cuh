@@ -56,12 +56,6 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&v)[16]) {
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
                    "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]) : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&v)[32]) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
-                 "tcgen05.wait::ld.sync.aligned;"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
-                 : "r"(taddr) : "memory");
-}
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&v)[64]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
                  "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
@@ -131,17 +125,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
-}
-// 2^x on the multipliers, for what the unit of ex2 has no time for: x is split into an integer and a rest in [-1/2, 1/2] (Cody and Waite's
-// reduction, by the rounding of an addition), 2^rest is a cubic (minimax of the relative error, 7.5e-5, by Remez exchange), the integer goes into
-// the exponent.  x <= 127; below -126 it counts as -126.  (17 values a clock and SM beside ex2's 16; the compiler pairs the additions and products.)
-__device__ __forceinline__ float exp2_cubic(float x) {
-    x = fmaxf(x, -126.f);
-    const float t = x + 12582912.f, f = x - (t - 12582912.f);
-    float p = fmaf(0.0551716685f, f, 0.2426111251f);
-    p = fmaf(p, f, 0.6932609677f);
-    p = fmaf(p, f, 0.9999280572f);
-    return __uint_as_float(__float_as_uint(p) + (__float_as_uint(t) << 23));
 }
 // the largest magnitudes so far of the bf16 values of 16 bytes, as bits; whether one of them is infinite or NaN
 __device__ __forceinline__ uint32_t bf16_magnitudes(uint32_t m, uint4 v) {
