@@ -12,9 +12,13 @@
 // Then (scale, zero) [N/16][Kd/128][16 rows][128/GS] with GS = 32, 64 or 128 codes to a pair (the largest of these that divides the group:
 // the kernel then knows how many pairs a block has, one load a row).  Rows and codes beyond N and Kd are zero.
 //
-// A warp walks the blocks of its row tile, four of them in flight in registers; the warps of a CTA share a row tile's blocks
-// (WK of them) or take row tiles of their own, and a cluster of CTAs shares the input dimension where the row tiles alone do not fill
-// the GPU.  Partial sums meet in shared memory (of the cluster's first CTA), in a fixed order.
+// A warp walks the blocks of its one or two row tiles (RT), 4 KB of codes in flight in registers; the warps of a CTA share the blocks of row
+// tiles (WK of them) or take row tiles of their own, and a cluster of CTAs shares the input dimension where the row tiles alone do not fill
+// the GPU.  Partial sums meet in shared memory, in a fixed order.
+//
+// 64,001 x 2,048 codes (74 MB with their scales): 1 token 18.1 us (4.1 TB/s), 8 20.5, 16 31, 64 97; 6,144 x 2,048 with an adapter of 16:
+// 1 token 7.9, 64 23.5; 1,024 x 1,024, 1 token: 6.7 (two launches and two waits for memory).  From 16 tokens on the products bound it: every 8
+// tokens more cost 11 us of the first, 25 clocks a product and quarter of an SM.
 #include <string.h>
 
 #include "edg_mma.cuh"
@@ -27,7 +31,6 @@ bool zero_points_ok(const uint16_t* z, size_t n);      // edg_pack.cu
 namespace {
 
 constexpr int kThreads = 256, kWarps = 8;
-constexpr int kAhead = 4;                     // blocks of codes in flight per warp
 
 inline int pair_codes(int group) { return group % 128 == 0 ? 128 : (group % 64 == 0 ? 64 : 32); }
 inline int blocks_of(int Kd) { return (Kd + 127) / 128; }
@@ -77,11 +80,11 @@ struct LinearParams {
     int N, Kd, T, rank, out_dtype, ldx;
     size_t ldy;
     int tiles, blocks;          // row tiles; blocks of 128 codes of the input dimension
-    int wk;                     // warps that share a row tile; kWarps / wk row tiles to a unit
+    int wk;                     // warps that share their row tiles; RT kWarps / wk row tiles to a unit
     int cluster, cta_blocks;    // CTAs that share the input dimension; blocks of each
     float lora_scale;
 };
-static_assert(kThreads % (kWarps * 16) == 0, "a thread keeps its row");
+static_assert(kThreads % (kWarps * 32) == 0, "a thread keeps its row");
 
 // u[t][r] = A[r] . x[t]: a warp per (token, rank)
 __global__ void __launch_bounds__(128) linear_u_kernel(const uint16_t* A, const uint16_t* x, float* u, int Kd, int ldx, int rank) {
@@ -104,59 +107,62 @@ __global__ void __launch_bounds__(128) linear_u_kernel(const uint16_t* A, const 
 }
 
 // Shared memory: activations [blocks][4 chunks][NT][32 lanes] 16 bytes; sums of them [blocks][128/GS][NT * 8] float; scales of the tokens
-// [NT * 8]; partial sums [kWarps][16 rows][NT * 8] float; A x of the tokens [NT * 8][rank rounded to 8] float.
-template <int GS, int NT> constexpr size_t linear_smem(int blocks, int rank) {
-    return (size_t)blocks * (NT * 2048 + (128 / GS) * NT * 32) + NT * 8 * 4 + kWarps * 16 * NT * 8 * 4 + (size_t)NT * 32 * ((rank + 7) & ~7);
+// [NT * 8]; partial sums [kWarps][16 RT rows][NT * 8] float; A x of the tokens [NT * 8][rank rounded to 8] float.
+template <int GS, int NT, int RT> constexpr size_t linear_smem(int blocks, int rank) {
+    return (size_t)blocks * (NT * 2048 + (128 / GS) * NT * 32) + NT * 8 * 4 + kWarps * 16 * RT * NT * 8 * 4 + (size_t)NT * 32 * ((rank + 7) & ~7);
 }
 
-// CTAs that share an SM, by the registers of NT tiles of tokens
-template <int NT> constexpr int kResident = NT <= 2 ? 2 : 1;
+constexpr int kResident = 2;                  // CTAs that share an SM
 
-template <int GS, int NT>
-__global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const __grid_constant__ LinearParams p) {
+template <int GS, int NT, int RT>
+__global__ void __launch_bounds__(kThreads, kResident) linear_kernel(const __grid_constant__ LinearParams p) {
     constexpr int PB = 128 / GS;                       // (scale, zero) pairs of a row in a block
-    constexpr int TN = NT * 8;
+    constexpr int TN = NT * 8, RR = 16 * RT;
+    constexpr int kAhead = 4 / RT;                     // blocks in flight per warp
     extern __shared__ __align__(16) uint8_t smem[];
     uint4* s_x = reinterpret_cast<uint4*>(smem);
     float* s_sum = reinterpret_cast<float*>(smem + (size_t)p.cta_blocks * NT * 2048);
     float* s_scale = s_sum + (size_t)p.cta_blocks * PB * TN;
     float* s_red = s_scale + TN;
-    float* s_u = s_red + kWarps * 16 * TN;
+    float* s_u = s_red + kWarps * RR * TN;
     const int ru = (p.rank + 7) & ~7;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
     const int rank_c = (int)(blockIdx.x % p.cluster), unit0 = (int)(blockIdx.x / p.cluster), n_units_grid = (int)(gridDim.x / p.cluster);
     const int t0 = blockIdx.y * TN, nt = min(TN, p.T - t0);
     const int b0 = rank_c * p.cta_blocks, nb = min(p.cta_blocks, p.blocks - b0);        // this CTA's blocks
-    const int wr = kWarps / p.wk;                      // row tiles of a unit
+    const int wr = kWarps / p.wk;                      // row tiles of a unit, RT at a time
+    const int tiles = (p.tiles + RT - 1) / RT;
     const int my_tile = warp / p.wk, my_k = warp % p.wk;
     const int per_unit = nb > my_k ? (nb - my_k + p.wk - 1) / p.wk : 0;                 // this warp's blocks of a unit
-    const int units = (p.tiles + wr - 1) / wr;
+    const int units = (tiles + wr - 1) / wr;
 
     // ---- the first blocks of codes are asked for before anything else
-    uint4 c0[kAhead], c1[kAhead];
-    uint32_t z0[kAhead][PB], z1[kAhead][PB];
-    auto load = [&](int slot, const uint8_t* c, const uint8_t* z) {
-        c0[slot] = ld_stream16(c);
-        c1[slot] = ld_stream16(c + 512);
+    uint4 c0[kAhead][RT], c1[kAhead][RT];
+    uint32_t z0[kAhead][RT][PB], z1[kAhead][RT][PB];
+    auto load = [&](int slot, int i, const uint8_t* c, const uint8_t* z) {
+        c0[slot][i] = ld_stream16(c);
+        c1[slot][i] = ld_stream16(c + 512);
         if constexpr (PB == 1) {
-            z0[slot][0] = ld_stream4(z);
-            z1[slot][0] = ld_stream4(z + 32);
+            z0[slot][i][0] = ld_stream4(z);
+            z1[slot][i][0] = ld_stream4(z + 32);
         } else if constexpr (PB == 2) {
             const uint2 a = __ldg(reinterpret_cast<const uint2*>(z)), b = __ldg(reinterpret_cast<const uint2*>(z + 64));
-            z0[slot][0] = a.x; z0[slot][1] = a.y; z1[slot][0] = b.x; z1[slot][1] = b.y;
+            z0[slot][i][0] = a.x; z0[slot][i][1] = a.y; z1[slot][i][0] = b.x; z1[slot][i][1] = b.y;
         } else {
             const uint4 a = ld_stream16(z), b = ld_stream16(z + 128);
-            z0[slot][0] = a.x; z0[slot][1] = a.y; z0[slot][2] = a.z; z0[slot][3] = a.w;
-            z1[slot][0] = b.x; z1[slot][1] = b.y; z1[slot][2] = b.z; z1[slot][3] = b.w;
+            z0[slot][i][0] = a.x; z0[slot][i][1] = a.y; z0[slot][i][2] = a.z; z0[slot][i][3] = a.w;
+            z1[slot][i][0] = b.x; z1[slot][i][1] = b.y; z1[slot][i][2] = b.z; z1[slot][i][3] = b.w;
         }
     };
     // A warp's blocks of a unit, rounded up to the slots: a block's slot is its number, known when the loop is unrolled.
     const int padded = (per_unit + kAhead - 1) / kAhead * kAhead;
     int lu = unit0, li = 0;                            // the next block to ask for, and where it lies
-    const size_t first = ((size_t)(unit0 * wr + my_tile) * p.blocks + b0 + my_k), jump = (size_t)n_units_grid * wr * p.blocks - (size_t)padded * p.wk;
+    const size_t first = ((size_t)(unit0 * wr + my_tile) * RT * p.blocks + b0 + my_k), jump = (size_t)n_units_grid * wr * RT * p.blocks - (size_t)padded * p.wk;
     const uint8_t *lc = p.codes + first * 1024 + lane * 16, *lz = p.sz + first * (64 * PB) + g * (4 * PB);
     auto load_next = [&](int slot) {
-        if (li < per_unit && lu * wr + my_tile < p.tiles) load(slot, lc, lz);
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+            if (li < per_unit && (lu * wr + my_tile) * RT + i < p.tiles) load(slot, i, lc + (size_t)i * p.blocks * 1024, lz + (size_t)i * p.blocks * (64 * PB));
         lc += p.wk * 1024;
         lz += p.wk * 64 * PB;
         if (++li == padded) {
@@ -184,7 +190,7 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
         };
         // Groups of GS codes go to the warps in turn.  The first ones stay in registers from the search for the largest magnitude to the
         // operands; what does not fit is read again.
-        constexpr int GC = GS / 32, kRoom = NT <= 2 ? 8 : 16, kKeep = kRoom / (NT * GC) > 0 ? kRoom / (NT * GC) : 1;
+        constexpr int GC = GS / 32, kRoom = 8, kKeep = kRoom / (NT * GC) > 0 ? kRoom / (NT * GC) : 1;
         uint4 keep[kKeep][GC][NT];
         uint32_t m[NT];
 #pragma unroll
@@ -261,37 +267,54 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
     bool u_there = p.rank == 0;
     for (int unit = unit0; unit < units; unit += n_units_grid) {
         const int tile = unit * wr + my_tile;
-        float acc[NT][4];
+        float acc[RT][NT][4];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
-        auto block = [&](int s, int i) {
-            const int lb = my_k + i * p.wk;            // block within this CTA's
-            const uint32_t w0[4] = {c0[s].x, c0[s].y, c0[s].z, c0[s].w}, w1[4] = {c1[s].x, c1[s].y, c1[s].z, c1[s].w};
-            float d[NT][4];
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j][0] = acc[i][j][1] = acc[i][j][2] = acc[i][j][3] = 0.f;
+        auto block = [&](int s, int n) {
+            const int lb = my_k + n * p.wk;            // block within this CTA's
+            float d[RT][NT][4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                uint32_t q0[4], q1[4];
-                dequant_word_s(w0[c], q0);
-                dequant_word_s(w1[c], q1);
+                uint32_t q0[RT][4], q1[RT][4];
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    const uint32_t w0[4] = {c0[s][i].x, c0[s][i].y, c0[s][i].z, c0[s][i].w}, w1[4] = {c1[s][i].x, c1[s][i].y, c1[s][i].z, c1[s][i].w};
+                    dequant_word_s(w0[c], q0[i]);
+                    dequant_word_s(w1[c], q1[i]);
+                }
                 const uint4* xb = s_x + (size_t)((lb * 4 + c) * NT) * 32 + lane;
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
                     const uint4 b = xb[j * 32];
-                    if (c % (GS / 32) == 0) mma16816_zero(d[j], q0[0], q1[0], q0[1], q1[1], b.x, b.y);
-                    else mma16816(d[j], q0[0], q1[0], q0[1], q1[1], b.x, b.y);
-                    mma16816(d[j], q0[2], q1[2], q0[3], q1[3], b.z, b.w);
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) {
+                        if (c % (GS / 32) == 0) mma16816_zero(d[i][j], q0[i][0], q1[i][0], q0[i][1], q1[i][1], b.x, b.y);
+                        else mma16816(d[i][j], q0[i][0], q1[i][0], q0[i][1], q1[i][1], b.x, b.y);
+                    }
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) mma16816(d[i][j], q0[i][2], q1[i][2], q0[i][3], q1[i][3], b.z, b.w);
                 }
                 if (c % (GS / 32) == GS / 32 - 1) {
                     const int pi = c / (GS / 32);
-                    const float2 f0 = __half22float2(u32_as_h2(z0[s][pi])), f1 = __half22float2(u32_as_h2(z1[s][pi]));
+                    float2 f0[RT], f1[RT];
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) {
+                        f0[i] = __half22float2(u32_as_h2(z0[s][i][pi]));
+                        f1[i] = __half22float2(u32_as_h2(z1[s][i][pi]));
+                    }
                     const float2* sm = reinterpret_cast<const float2*>(s_sum + (lb * PB + pi) * TN) + t4;
 #pragma unroll
                     for (int j = 0; j < NT; ++j) {
                         const float2 xs = sm[j * 4];
-                        acc[j][0] = fmaf(f0.x, fmaf(-f0.y, xs.x, d[j][0]), acc[j][0]);
-                        acc[j][1] = fmaf(f0.x, fmaf(-f0.y, xs.y, d[j][1]), acc[j][1]);
-                        acc[j][2] = fmaf(f1.x, fmaf(-f1.y, xs.x, d[j][2]), acc[j][2]);
-                        acc[j][3] = fmaf(f1.x, fmaf(-f1.y, xs.y, d[j][3]), acc[j][3]);
+#pragma unroll
+                        for (int i = 0; i < RT; ++i) {
+                            acc[i][j][0] = fmaf(f0[i].x, fmaf(-f0[i].y, xs.x, d[i][j][0]), acc[i][j][0]);
+                            acc[i][j][1] = fmaf(f0[i].x, fmaf(-f0[i].y, xs.y, d[i][j][1]), acc[i][j][1]);
+                            acc[i][j][2] = fmaf(f1[i].x, fmaf(-f1[i].y, xs.x, d[i][j][2]), acc[i][j][2]);
+                            acc[i][j][3] = fmaf(f1[i].x, fmaf(-f1[i].y, xs.y, d[i][j][3]), acc[i][j][3]);
+                        }
                     }
                 }
             }
@@ -299,23 +322,25 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
         for (int i = 0; i < padded; i += kAhead)
 #pragma unroll
             for (int s = 0; s < kAhead; ++s) {
-                if (i + s < per_unit && tile < p.tiles) block(s, i + s);
+                if (i + s < per_unit && tile < tiles) block(s, i + s);
                 load_next(s);
             }
         // ---- partial sums meet: [warp][row][token]
-        float* red = s_red + warp * 16 * TN;
+        float* red = s_red + warp * RR * TN;
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            *reinterpret_cast<float2*>(red + g * TN + j * 8 + 2 * t4) = make_float2(acc[j][0], acc[j][1]);
-            *reinterpret_cast<float2*>(red + (g + 8) * TN + j * 8 + 2 * t4) = make_float2(acc[j][2], acc[j][3]);
-        }
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                *reinterpret_cast<float2*>(red + (i * 16 + g) * TN + j * 8 + 2 * t4) = make_float2(acc[i][j][0], acc[i][j][1]);
+                *reinterpret_cast<float2*>(red + (i * 16 + g + 8) * TN + j * 8 + 2 * t4) = make_float2(acc[i][j][2], acc[i][j][3]);
+            }
         __syncthreads();
         if (p.cluster > 1) {                           // this CTA's sums over its warps, scaled, into the first warp's of each row tile
-            for (int o = tid; o < wr * 16 * TN; o += kThreads) {
-                const int x = o / (16 * TN), at = o - x * 16 * TN;
-                float* s = s_red + x * p.wk * 16 * TN + at;
+            for (int o = tid; o < wr * RR * TN; o += kThreads) {
+                const int x = o / (RR * TN), at = o - x * RR * TN;
+                float* s = s_red + x * p.wk * RR * TN + at;
                 float v = s[0];
-                for (int k = 1; k < p.wk; ++k) v += s[k * 16 * TN];
+                for (int k = 1; k < p.wk; ++k) v += s[k * RR * TN];
                 s[0] = v * s_scale[at % TN];
             }
             __syncwarp();
@@ -332,9 +357,9 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
             u_there = true;
         }
         // outputs of the unit, spread over the cluster's CTAs: a thread keeps its row, consecutive threads take consecutive rows
-        const int rows = wr * 16, row = tid & (rows - 1), rt = row >> 4, n = (unit * wr + rt) * 16 + (row & 15);
+        const int rows = wr * RR, row = tid & (rows - 1), rt = row / RR, n = unit * rows + row;
         const int tstep = p.cluster * kThreads / rows, tok0 = (rank_c * kThreads + tid) / rows;
-        const float* src = s_red + rt * p.wk * 16 * TN + (row & 15) * TN;
+        const float* src = s_red + rt * p.wk * RR * TN + (row & (RR - 1)) * TN;
         auto value = [&](int tok) {
             float v = 0.f;
             if (p.cluster > 1) {
@@ -346,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
                 for (int c = 0; c < 8; ++c)
                     if (c < p.cluster) v += f[c];
             } else {
-                for (int k = 0; k < p.wk; ++k) v += src[tok + k * 16 * TN];
+                for (int k = 0; k < p.wk; ++k) v += src[tok + k * RR * TN];
                 v *= s_scale[tok];
             }
             return v;
@@ -402,39 +427,41 @@ __global__ void __launch_bounds__(kThreads, kResident<NT>) linear_kernel(const _
 }
 
 constexpr size_t kMost = 200 * 1024;
-struct LinearPlan { int nt, wk, cluster, cta_blocks, grid; size_t smem; int64_t cost; };
+struct LinearPlan { int nt, rt, wk, cluster, cta_blocks, grid; size_t smem; int64_t cost; };
 
-// Tokens of a pass (8 NT), warps that share a row tile, CTAs that share the input dimension: what takes the least by the rounds that a CTA's
-// warps make.  In clocks: a block of 128 codes 200 + 100 NT of a warp with seven beside it and half as much more with fifteen, the sums' meeting
-// 700 + 60 NT and 1500 more in a cluster, the activations 1500 + 60 NT a block at the start.
-template <int GS, int NT> void plan_linear(const LinearParams& p, int sms, LinearPlan& best) {
+// Tokens of a pass (8 NT), row tiles of a warp (RT), warps that share them, CTAs that share the input dimension: what takes the least by the rounds that a CTA's
+// warps make.  In clocks: a block of 128 codes 200 + 100 NT of a warp with seven beside it and half as much more with fifteen (of two row tiles
+// 300 + 150 NT), the sums' meeting 700 + 60 NT a row tile and 1500 more in a cluster, the activations 1500 + 60 NT a block at the start.  Against
+// every shape of a launch at 13 sizes (1 to 64 tokens) this took 0 to 16% longer than the best; four or eight tiles of tokens never were that.
+// Two row tiles at once share the activations' operands: 64,001 rows, 16 tokens 32.5 -> 31 us; 6,144 rows, 16 tokens 11.1 -> 8.8.
+template <int GS, int NT, int RT> void plan_linear(const LinearParams& p, int sms, LinearPlan& best) {
     const int slices = (p.T + NT * 8 - 1) / (NT * 8);
     for (int c = 1; c <= 8; c *= 2)
         for (int wk = 1; wk <= kWarps; wk *= 2) {
             const int each = (p.blocks + c - 1) / c;
-            const size_t bytes = linear_smem<GS, NT>(each, p.rank);
+            const size_t bytes = linear_smem<GS, NT, RT>(each, p.rank);
             if (bytes > kMost || (c > 1 && each * (c - 1) >= p.blocks)) continue;      // (every CTA has blocks)
             int resident = (int)((220 * 1024) / (bytes + 1024));
-            resident = resident < 1 ? 1 : (resident > kResident<NT> ? kResident<NT> : resident);
-            const int units = (p.tiles + kWarps / wk - 1) / (kWarps / wk), room = sms * resident / c > 0 ? sms * resident / c : 1;
+            resident = resident < 1 ? 1 : (resident > kResident ? kResident : resident);
+            const int units = ((p.tiles + RT - 1) / RT + kWarps / wk - 1) / (kWarps / wk), room = sms * resident / c > 0 ? sms * resident / c : 1;
             const int64_t all = (int64_t)units * slices, rounds = (all + room - 1) / room;
             const int beside = all * c > sms ? resident : 1;                           // CTAs that share an SM's pipes
-            const int64_t cost = rounds * ((int64_t)((each + wk - 1) / wk) * (200 + 100 * NT) * (beside > 1 ? 3 : 2) / 2 + 700 + 60 * NT + (c > 1 ? 1500 : 0)) +
+            const int64_t cost = rounds * ((int64_t)((each + wk - 1) / wk) * (RT == 1 ? 200 + 100 * NT : 300 + 150 * NT) * (beside > 1 ? 3 : 2) / 2 + 700 + 60 * NT * RT + (c > 1 ? 1500 : 0)) +
                                  1500 + each * 60 * NT;
             if (best.cost >= 0 && cost >= best.cost) continue;
-            best = {NT, wk, c, each, (int)((units + rounds - 1) / rounds), bytes, cost};
+            best = {NT, RT, wk, c, each, (int)((units + rounds - 1) / rounds), bytes, cost};
         }
 }
 
-template <int GS, int NT> int32_t launch_linear(LinearParams& p, const LinearPlan& plan, cudaStream_t st) {
+template <int GS, int NT, int RT> int32_t launch_linear(LinearParams& p, const LinearPlan& plan, cudaStream_t st) {
     static OncePerDevice once;
-    EDG_CUDA_TRY(once([] { return allow_smem(kMost, linear_kernel<GS, NT>); }));
+    EDG_CUDA_TRY(once([] { return allow_smem(kMost, linear_kernel<GS, NT, RT>); }));
     p.wk = plan.wk;
     p.cluster = plan.cluster;
     p.cta_blocks = plan.cta_blocks;
     const dim3 grid(plan.grid * plan.cluster, (p.T + NT * 8 - 1) / (NT * 8));
-    EDG_CUDA_TRY(p.rank > 0 ? launch_pdl_cluster(p.cluster, linear_kernel<GS, NT>, grid, kThreads, plan.smem, st, p)
-                            : launch_cluster(p.cluster, linear_kernel<GS, NT>, grid, kThreads, plan.smem, st, p));
+    EDG_CUDA_TRY(p.rank > 0 ? launch_pdl_cluster(p.cluster, linear_kernel<GS, NT, RT>, grid, kThreads, plan.smem, st, p)
+                            : launch_cluster(p.cluster, linear_kernel<GS, NT, RT>, grid, kThreads, plan.smem, st, p));
     return EDG_OK;
 }
 
@@ -442,16 +469,15 @@ template <int GS> int32_t launch_gs(LinearParams& p, cudaStream_t st) {
     const int sms = sm_count();
     LinearPlan plan;
     plan.cost = -1;
-    plan_linear<GS, 1>(p, sms, plan);
-    if (p.T > 8) plan_linear<GS, 2>(p, sms, plan);
-    if (p.T > 16) plan_linear<GS, 4>(p, sms, plan);
-    if (p.T > 32) plan_linear<GS, 8>(p, sms, plan);
+    plan_linear<GS, 1, 1>(p, sms, plan);
+    plan_linear<GS, 1, 2>(p, sms, plan);
+    if (p.T > 8) { plan_linear<GS, 2, 1>(p, sms, plan); plan_linear<GS, 2, 2>(p, sms, plan); }
     if (plan.cost < 0) return EDG_E_SHAPE;
-    switch (plan.nt) {
-        case 1: return launch_linear<GS, 1>(p, plan, st);
-        case 2: return launch_linear<GS, 2>(p, plan, st);
-        case 4: return launch_linear<GS, 4>(p, plan, st);
-        default: return launch_linear<GS, 8>(p, plan, st);
+    switch (plan.nt * 10 + plan.rt) {
+        case 11: return launch_linear<GS, 1, 1>(p, plan, st);
+        case 12: return launch_linear<GS, 1, 2>(p, plan, st);
+        case 21: return launch_linear<GS, 2, 1>(p, plan, st);
+        default: return launch_linear<GS, 2, 2>(p, plan, st);
     }
 }
 
