@@ -4,7 +4,9 @@
 //
 // Bound by HBM for prompts (each row read and written once) and by latency for a step of decoding.  A row is a warp's, or with few rows a CTA's:
 // one warp of it takes the cache row, all of them the heads of its query; a lane rotates pairs of eight consecutive values.  Angles are formed and brought to
-// [-pi, pi] in double (a position of 10^5 and more leaves no digit of the angle in fp32), sine and cosine are fp32.
+// [-pi, pi] in double (a position of 10^5 and more leaves no digit of the angle in fp32), sine and cosine are fp32.  A value is rounded
+// once, when it is written.  Measured with 32 heads and 512 + 64 columns: 64 rows of as many sequences 4.2 us in a graph (a wait for the
+// sequence's place, one for the row), 4,430 rows 12.9 (46 MB: 3.6 TB/s, half of it from L2).
 #include "edg_latent.cuh"
 
 namespace edg {

@@ -13,6 +13,10 @@
 // after that takes what S has read).  Positions behind a sequence's end are padded to 128; their values are written as zeros, their scores
 // never looked at.
 //
+// K, V and P are rounded to bf16, by 2^-8 of a value at most: the operands of a product have one type, the cache's is bf16, and fp16
+// would not hold its range.  Maxima, sums and O are fp32.  Of a standard normal batch the outputs before their own rounding are 0.2% off in the
+// mean square.
+//
 // 4,430 new rows of three sequences of 7,103 positions, 32 heads of 128 + 64 / 128, 512 latent columns: expand_kernel 62 us (62 GFLOP: 1.0
 // PFLOP/s; its limits are the weights, which every CTA reads from L2, and its two rounds of CTAs), prompt_kernel 182 us (185 GFLOP of rows that
 // see one another: 1.0 PFLOP/s).  A pair of tiles takes 3,900 clocks of which the tensor cores work 3,260; S of a tile, its softmax (2,050), P V
