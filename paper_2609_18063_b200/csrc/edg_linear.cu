@@ -19,6 +19,7 @@
 // 64,001 x 2,048 codes (74 MB with their scales): 1 token 18.1 us (4.1 TB/s), 8 20.5, 16 31, 64 97; 6,144 x 2,048 with an adapter of 16:
 // 1 token 7.9, 64 23.5; 1,024 x 1,024, 1 token: 6.7 (two launches and two waits for memory).  From 16 tokens on the products bound it: every 8
 // tokens more cost 11 us of the first, 25 clocks a product and quarter of an SM.
+#include <cooperative_groups.h>
 #include <string.h>
 
 #include "edg_mma.cuh"
@@ -27,6 +28,8 @@
 namespace edg {
 
 bool zero_points_ok(const uint16_t* z, size_t n);      // edg_pack.cu
+
+namespace cg = cooperative_groups;
 
 namespace {
 
@@ -359,6 +362,7 @@ __global__ void __launch_bounds__(kThreads, kResident) linear_kernel(const __gri
         // outputs of the unit, spread over the cluster's CTAs: a thread keeps its row, consecutive threads take consecutive rows
         const int rows = wr * RR, row = tid & (rows - 1), rt = row / RR, n = unit * rows + row;
         const int tstep = p.cluster * kThreads / rows, tok0 = (rank_c * kThreads + tid) / rows;
+        const cg::cluster_group cluster = cg::this_cluster();
         const float* src = s_red + rt * p.wk * RR * TN + (row & (RR - 1)) * TN;
         auto value = [&](int tok) {
             float v = 0.f;
@@ -366,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, kResident) linear_kernel(const __gri
                 float f[8];
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
-                    if (c < p.cluster) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f[c]) : "r"(map_to_cta(src + tok, c)));
+                    if (c < p.cluster) f[c] = *cluster.map_shared_rank(src + tok, c);
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
                     if (c < p.cluster) v += f[c];
