@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(o_empty + 1);
     float* s_alpha = reinterpret_cast<float*>(smem + P::alpha);
     float* s_most = reinterpret_cast<float*>(smem + P::most);             // [2][half of the columns][row]
-    __shared__ long long s_tiles[kThreads / 32], s_from[2];
+    __shared__ long long s_tiles[kThreads / 32], s_fresh[kThreads / 32], s_from[2];
     __shared__ int s_units[kThreads / 32], s_at[3];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g = blockIdx.x / p.group, r = blockIdx.x % p.group;
@@ -280,12 +280,13 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
     // ---- this group's stretch of the line of tiles, and the sequence it begins in
     {
         const int per = (p.s.n + kThreads - 1) / kThreads, i0 = min(tid * per, p.s.n), i1 = min(i0 + per, p.s.n);
-        long long t = 0;
+        long long t = 0, fresh = 0;
         int u = 0;
         for (int i = i0; i < i1; ++i) {
             const Seq q = sequence(p, i);
             t += q.units * unit_length(q);
             u += q.units;
+            fresh += q.fresh;
         }
         long long xt = t;
         int xu = u;
@@ -294,17 +295,20 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
             const long long yt = __shfl_up_sync(0xFFFFFFFFu, xt, o);
             const int yu = __shfl_up_sync(0xFFFFFFFFu, xu, o);
             if (lane >= o) { xt += yt; xu += yu; }
+            fresh += __shfl_xor_sync(0xFFFFFFFFu, fresh, o);
         }
-        if (lane == 31) { s_tiles[warp] = xt; s_units[warp] = xu; }
+        if (lane == 31) { s_tiles[warp] = xt; s_units[warp] = xu; s_fresh[warp] = fresh; }
         tc_fence_before();
         __syncthreads();
         tc_fence_after();
-        long long W = 0, before = xt - t;
+        long long W = 0, before = xt - t, all_fresh = 0;
         int ub = xu - u;
         for (int w = 0; w < kThreads / 32; ++w) {
             if (w < warp) { before += s_tiles[w]; ub += s_units[w]; }
             W += s_tiles[w];
+            all_fresh += s_fresh[w];
         }
+        if (all_fresh > p.s.T) W = 0;                                    // (sequences that overlap: reported, and no end of work otherwise)
         const long long each = stretch(W, p.groups), start = min(each * g, W), end = min(start + each, W);
         if (tid == 0) { s_from[1] = end - start; if (end <= start) { s_from[0] = 0; s_at[0] = s_at[1] = s_at[2] = 0; } }
         if (end > start && t > 0 && before <= start && start < before + t) {
@@ -706,7 +710,7 @@ __global__ void __launch_bounds__(kCombine, 1) combine_kernel(const __grid_const
                 const long long each = stretch(W, p.groups), at = before + ug * unit_length(q) + kPiece;
                 const int g0 = (int)quotient(at, each), g1 = (int)quotient(at + q.kt - 1, each);
                 first = g0 + units + ug;
-                count = max(min(g1 - g0 + 1, p.max_slots - first), 0);
+                count = first >= 0 ? max(min(g1 - g0 + 1, p.max_slots - first), 0) : 0;
             }
         }
         const size_t step = (size_t)p.group * p.R, at = (size_t)first * step + row;

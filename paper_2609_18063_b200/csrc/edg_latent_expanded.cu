@@ -61,16 +61,17 @@ __global__ void __launch_bounds__(256) prompt_plan_kernel(const __grid_constant_
     pdl_launch_dependents();
     if (threadIdx.x == 0) *p.next = 0;
     __shared__ int s_q[8], s_k[8];
-    __shared__ long long s_l[8];
+    __shared__ long long s_l[8], s_f[8];
     const int tid = threadIdx.x, per = (p.s.n + 255) / 256, i0 = min(tid * per, p.s.n), i1 = min(i0 + per, p.s.n);
     int q = 0, k = 0;
-    long long len = 0;
+    long long len = 0, fresh = 0;
     bool ok = tid != 0 || (p.s.cu[0] == 0 && p.s.cu[p.s.n] <= p.s.T);
     for (int i = i0; i < i1; ++i) {
         const XSeq x = xsequence(p, i);
         q += x.pairs;
         k += x.tiles;
         len += x.len;
+        fresh += x.fresh;
         ok = ok && p.s.cu[i + 1] >= p.s.cu[i] && x.fresh <= p.max_new && x.len >= p.s.lens[i];
     }
     const int lane = tid & 31, warp = tid >> 5, own_q = q, own_k = k;
@@ -79,20 +80,25 @@ __global__ void __launch_bounds__(256) prompt_plan_kernel(const __grid_constant_
         const int a = __shfl_up_sync(0xFFFFFFFFu, q, d), b = __shfl_up_sync(0xFFFFFFFFu, k, d);
         if (lane >= d) { q += a; k += b; }
         len += __shfl_xor_sync(0xFFFFFFFFu, len, d);
+        fresh += __shfl_xor_sync(0xFFFFFFFFu, fresh, d);
     }
-    if (lane == 31) { s_q[warp] = q; s_k[warp] = k; s_l[warp] = len; }
+    if (lane == 31) { s_q[warp] = q; s_k[warp] = k; s_l[warp] = len; s_f[warp] = fresh; }
     __syncthreads();
     q -= own_q;
     k -= own_k;
-    len = 0;
+    len = fresh = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         if (j < warp) { q += s_q[j]; k += s_k[j]; }
         len += s_l[j];
+        fresh += s_f[j];
     }
     if (!ok || len > p.total_len) latent_raise(p.status, EDG_E_RANGE);
+    const bool none = len > p.total_len || fresh > p.s.T;                // (sequences that overlap, or more than there is room for: nothing is done)
+    if (none) q = k = 0;
     for (int i = i0; i < i1; ++i) {
-        const XSeq x = xsequence(p, i);
+        XSeq x = xsequence(p, i);
+        if (none) x.pairs = x.tiles = 0;
         p.q_pre[i] = q;
         p.kv_pre[i] = k;
         q += x.pairs;
@@ -496,14 +502,14 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
             };
             // ---- work: the last pairs of a sequence see the most, they go first.  (The next one is taken when all of this one's loads are on their
             // way, not before: taken a whole pair ahead, the last CTA had 82 of 67 tiles on average.)
-            const int total = p.q_pre[p.s.n] * p.heads;
+            const int pairs = p.q_pre[p.s.n], total = pairs * p.heads;
             auto next_item = [&]() {
                 int w = 0;
                 if (lane == 0) w = atomicAdd(p.next, 1);
                 w = __shfl_sync(0xFFFFFFFFu, w, 0);
                 x.h = -1;
                 if (w >= 0 && w < total) {
-                    const int pair = total / p.heads - 1 - w / p.heads, seq = min(find_sequence(p.q_pre, p.s.n, pair, lane), p.s.n - 1);
+                    const int pair = pairs - 1 - w / p.heads, seq = min(find_sequence(p.q_pre, p.s.n, pair, lane), p.s.n - 1);
                     const XSeq q = xsequence(p, seq);
                     const int r0 = (pair - p.q_pre[seq]) * 256;
                     x.h = w % p.heads;
