@@ -6,7 +6,7 @@
 // one warp of it takes the cache row, all of them the heads of its query; a lane rotates pairs of eight consecutive values.  Angles are formed and brought to
 // [-pi, pi] in double (a position of 10^5 and more leaves no digit of the angle in fp32), sine and cosine are fp32.  A value is rounded
 // once, when it is written.  Measured with 32 heads and 512 + 64 columns: 64 rows of as many sequences 4.2 us in a graph (a wait for the
-// sequence's place, one for the row), 4,430 rows 12.9 (46 MB: 3.6 TB/s, half of it from L2).
+// sequence's place, one for the row), 4,430 rows 10.6 (46 MB: 4.3 TB/s, half of it from L2; 16.4 with all of it from memory).
 #include "edg_latent.cuh"
 
 namespace edg {
@@ -58,12 +58,14 @@ __device__ __forceinline__ void rotate8(const uint4& in, uint16_t* out, int j, i
     }
 }
 
-constexpr int kPieces = 8;                    // 16-byte pieces of queries that a lane has in flight
+// 16-byte pieces of queries that a lane has in flight.  (With eight a thread needs 79 registers, and 4,430 rows take the warps of an SM a second
+// time round: 13.3 us instead of 10.6.)
+constexpr int kPieces = 4;
 
 // WARPS: warps that share a row.  All that does not depend on the row's place is asked for first: the search for the sequence, its length, its
 // page and the angles are a chain of four trips to memory, and run beside it.
 template <int WARPS>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const __grid_constant__ AppendParams p) {
     constexpr int kRows = kAppendThreads / 32 / WARPS;
     __shared__ float2 s_cs[kAppendThreads / 32][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = blockIdx.x * kRows + warp / WARPS, share = warp % WARPS;
@@ -180,7 +182,8 @@ extern "C" int32_t latent_append(const edg_latent_desc* desc, int32_t n_seqs, in
     p.ldq = latent_ldq(*desc);
     p.halves = desc->rope_halves;
     p.eps = eps;
-    // Few rows: the warps of a CTA share one; many: a warp each (4430 rows of 32 heads 15.9 -> 12.9 us in a graph, 64 rows the other way round).
+    // Few rows: the warps of a CTA share one; many: a warp each (4430 rows of 32 heads 10.6 us in a graph, with two warps to a row 11.9, with four
+    // 14.0; 64 rows the other way round).
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (T < 1024) append_kernel<8><<<T, kAppendThreads, 0, st>>>(p);
     else append_kernel<1><<<(T + 7) / 8, kAppendThreads, 0, st>>>(p);
