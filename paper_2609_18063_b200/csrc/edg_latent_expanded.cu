@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
             const uint32_t st = tmem + ((uint32_t)(wq * 32) << 16) + i * 128, ot = st + 256;
             const float k2 = p.scale * 1.4426950408889634f;
             float* my_max = s_max + (i * 2 + half) * 128 + wq * 32 + lane;
-            const float* their_max = s_max + (i * 2 + 1 - half) * 128 + wq * 32 + lane;
+            float* their_max = s_max + (i * 2 + 1 - half) * 128 + wq * 32 + lane;
             uint32_t done = 0;                                           // tiles, of all items
             Item x;
             while (take_item(x)) {
@@ -445,9 +445,11 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                     }
                 continue;
             }
-            *my_max = l;
+            // (A sum goes to the place of the other half's maximum, whose one reader is this thread: behind the last tile nothing tells that the
+            // other has read this one's.)
+            *their_max = l;
             barrier_sync(1 + i, 256);
-            l += *their_max;
+            l += *my_max;
             barrier_sync(1 + i, 256);                                    // (the next item's maxima go there)
             const float inv = l == 0.f ? 0.f : 1.f / l;
             role_wait(&o_done[i], (done - 1) & 1, p.status);
