@@ -395,6 +395,11 @@ __global__ void __launch_bounds__(kThreads, 1) absorbed_kernel(const __grid_cons
             }
         }
         if (!waited) pdl_wait_prior_grid();
+        if (half == 0) {                                                 // (no arrival of a product may come after the block's end)
+            for (int i = 0; i < P::NV; ++i, v.next(P::NV)) role_wait(&v_empty[v.slot], v.phase ^ 1, p.status);
+            for (int i = 0; i < P::NR; ++i, ro.next(P::NR)) role_wait(&r_empty[ro.slot], ro.phase ^ 1, p.status);
+            role_wait(q_empty, q_phase, p.status);
+        }
     } else if (warp == 1) {
         // ============================================= S of every tile, in two halves as they arrive.  (O is another warp's: what queues up
         // behind a product covers two or three of them, a wait costs as much, and each warp's products cover the other's waits.)

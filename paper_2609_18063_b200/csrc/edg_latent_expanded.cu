@@ -186,6 +186,8 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
                             w.next(kXRing);
                         }
                     }
+                // (no arrival of a product may come after the block's end)
+                for (int i = 0; i < kXRing; ++i, w.next(kXRing)) role_wait(&w_empty[w.slot], w.phase ^ 1, p.status);
             }
             __syncwarp();
         } else if (warp == 1) {
@@ -562,6 +564,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
             }
             }
             while (held > 0) room_left();                                // (no arrival may come after the block's end)
+            for (int i = 0; i < 2; ++i) role_wait(&q_empty[i], (begun[i] & 1) ^ 1, p.status);
         } else if (warp == 1) {
             // ========================================= products, by one thread: for each tile of rows O += P V of a tile of positions, then S of the
             // next.  (What it does between two products is time in which the tensor cores wait: they hold two or three products of 65 clocks.)

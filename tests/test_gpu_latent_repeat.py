@@ -28,3 +28,10 @@ def test_the_two_threads_of_a_row_exchange_maxima_and_then_sums(new):
 
 def test_the_two_threads_of_a_row_where_cached_positions_lie_before_the_prompt():
     _again(Batch(LARGE, [100] * 40, [100 + 61 * i for i in range(40)], form=edg.LATENT_EXPANDED, page=128))
+
+
+@pytest.mark.parametrize("form", [edg.LATENT_ABSORBED, edg.LATENT_EXPANDED])
+@pytest.mark.parametrize("heads,new,lens", [(8, [1], [1]), (24, [1, 1], [70, 5]), (8, [9, 1], [64, 130]), (8, [3] * 150, [3 + i % 140 for i in range(150)])])
+def test_blocks_that_end_with_their_first_tiles(form, heads, new, lens):
+    """A block waits for all arrivals of its products before it ends: launches of a tile or two in a row, none behind the other's barriers."""
+    _again(Batch(dict(SMALL, heads=heads), new, lens, form=form, page=16))
