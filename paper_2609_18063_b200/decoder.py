@@ -83,23 +83,47 @@ class LatentCache:
         return B.workspace_status(self.ws)
 
 
+def _refuse(bad: bool, what: str) -> None:
+    if bad:
+        raise ValueError(what)
+
+
+def _is(t, shape, dtype, device) -> bool:
+    """Whether t is a tensor like that (an address says nothing about itself: taken as given)."""
+    return not isinstance(t, torch.Tensor) or (tuple(t.shape) == tuple(shape) and t.dtype == dtype and t.device == device)
+
+
 class LatentBlock:
     """The attention half of one decoder layer: int4 projections of the hidden state to queries and latent rows, latent attention over the
     request's pages, int4 output projection.  Serves single tokens, batches of requests and prompts alike.
 
     ``w_q``, ``w_kv``, ``w_out``: (LinearDesc, device record) with N = heads * (d_nope + d_rope), d_latent + d_rope and H; ``w_uk`` / ``w_uv`` device
     bf16 [heads][d_nope][d_latent] / [heads][d_v][d_latent]; ``gain`` device bf16 [d_latent] or None; ``inv_freq`` device f32 [d_rope / 2].
-    Adapters: an optional (A, B) behind the record."""
+    Adapters: an optional (A, B) behind the record.  Rows of all of them are dense.  What one call writes and the next reads is bf16: the outputs of
+    ``w_q`` and ``w_kv``, and ``desc``'s; ``w_out`` writes any type.  Anything else is a ValueError."""
 
     def __init__(self, desc: B.LatentDesc, w_q, w_kv, w_out, w_uk, w_uv, gain, inv_freq, max_rows: int, max_seqs: int, max_new: int, max_total: int):
         self.desc, self.w_q, self.w_kv, self.w_out = desc, w_q, w_kv, w_out
         self.w_uk, self.w_uv, self.gain, self.inv_freq = w_uk, w_uv, gain, inv_freq
-        h, dev = desc.heads, w_uk.device
-        half = {B.F16: torch.float16, B.BF16: torch.bfloat16}[desc.out_dtype]
+        h, dev, bf16 = desc.heads, w_uk.device, torch.bfloat16
+        d_q, d_kv, H = h * (desc.d_nope + desc.d_rope), desc.d_latent + desc.d_rope, w_q[0].Kd
+        _refuse(desc.out_dtype != B.BF16, "the output projection reads bf16: out_dtype of the attention must be bf16")
+        _refuse(desc.ldq not in (0, d_q) or desc.ldkv not in (0, d_kv), "a block's queries and rows lie dense")
+        for name, w, N, Kd, out in (("w_q", w_q, d_q, H, B.BF16), ("w_kv", w_kv, d_kv, H, B.BF16), ("w_out", w_out, H, h * desc.d_v, None)):
+            d = w[0]
+            _refuse((d.N, d.Kd) != (N, Kd), f"{name} is {d.N} x {d.Kd}, the block needs {N} x {Kd}")
+            _refuse(out is not None and d.out_dtype != out, f"{name} must write bf16")
+            _refuse(d.ldx not in (0, Kd) or d.ldy not in (0, N), f"{name}: a block's rows lie dense")
+            _refuse(isinstance(w[1], torch.Tensor) and (w[1].device != dev or w[1].nbytes < B.linear_record_bytes(d)), f"{name}: not a record of this projection")
+            _refuse(len(w) not in (2, 4) or (d.rank > 0) != (len(w) == 4), f"{name}: an adapter where the rank is not 0, and none elsewhere")
+            _refuse(len(w) == 4 and not (_is(w[2], (d.rank, Kd), bf16, dev) and _is(w[3], (N, d.rank), bf16, dev)), f"{name}: A [rank][Kd] and B [N][rank] in bf16")
+        _refuse(not _is(w_uk, (h, desc.d_nope, desc.d_latent), bf16, dev) or not _is(w_uv, (h, desc.d_v, desc.d_latent), bf16, dev), "w_uk and w_uv")
+        _refuse(gain is not None and not _is(gain, (desc.d_latent,), bf16, dev), "gain")
+        _refuse(not _is(inv_freq, (desc.d_rope // 2,), torch.float32, dev), "inv_freq")
         self.q = torch.empty((max_rows, h * (desc.d_nope + desc.d_rope)), dtype=torch.bfloat16, device=dev)
         self.kv = torch.empty((max_rows, desc.d_latent + desc.d_rope), dtype=torch.bfloat16, device=dev)
         self.q_rope = torch.empty((max_rows, h, desc.d_rope), dtype=torch.bfloat16, device=dev)
-        self.a = torch.empty((max_rows, h * desc.d_v), dtype=half, device=dev)
+        self.a = torch.empty((max_rows, h * desc.d_v), dtype=torch.bfloat16, device=dev)
         self.bounds = (max_seqs, max_rows, max_new, max_total)
         self.ws = torch.zeros(B.latent_workspace_bytes(desc, *self.bounds), dtype=torch.uint8, device=dev)
         need = max(B.linear_workspace_bytes(w[0], max_rows) for w in (w_q, w_kv, w_out))
