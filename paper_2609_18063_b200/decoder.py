@@ -83,6 +83,9 @@ class LatentCache:
         return B.workspace_status(self.ws)
 
 
+_TYPES = {B.F32: torch.float32, B.F16: torch.float16, B.BF16: torch.bfloat16}
+
+
 def _refuse(bad: bool, what: str) -> None:
     if bad:
         raise ValueError(what)
@@ -135,9 +138,22 @@ class LatentBlock:
 
     def run(self, x, y, cu, lens, table, rows, max_new=1, total=None, eps=1e-6) -> None:
         """x device bf16 [T][H] (the new rows of n = cu.numel() - 1 sequences, whose places in the cache are reserved), y device [T][H] of
-        ``w_out``'s type; lens and table are those of the same n sequences, rows the layer's part of the cache; total bounds the sum of lens."""
-        n, T = cu.numel() - 1, x.shape[0]
+        ``w_out``'s type; cu, lens and table (int32) are those of the same n sequences, rows the layer's part of the cache; max_new bounds the new
+        rows of a sequence, total the sum of lens.  What exceeds the block's own bounds, or does not fit it, is a ValueError, and nothing is launched."""
+        n, T, d = cu.numel() - 1, x.shape[0], self.desc
         total = self.bounds[3] if total is None else total
+        out, dev, i32 = self.w_out[0], self.w_uk.device, torch.int32
+        if not (1 <= n <= self.bounds[0] and 1 <= T <= self.bounds[1] and 1 <= max_new <= min(self.bounds[2], T) and 0 <= total <= self.bounds[3]):
+            raise ValueError(f"{n} sequences, {T} rows, {max_new} of one sequence, {total} positions: the block is made for {self.bounds}")
+        if not _is(x, (T, self.w_q[0].Kd), torch.bfloat16, dev) or y.numel() != T * out.N or y.dtype != _TYPES[out.out_dtype] or y.device != dev:
+            raise ValueError("x is bf16 [T][H], y [T][H] of the output projection's type")
+        if not (cu.dtype == lens.dtype == table.dtype == i32 and cu.device == lens.device == table.device == dev and lens.numel() >= n
+                and table.dim() == 2 and table.shape[0] >= n and table.shape[1] == d.max_pages):
+            raise ValueError("cu, lens and table are int32 [n + 1], [n] and [n][max_pages]")
+        if not _is(rows, (d.n_pages, d.page, d.d_latent + d.d_rope), torch.bfloat16, dev):
+            raise ValueError("rows are the layer's bf16 [n_pages][page][d_latent + d_rope]")
+        if not (x.is_contiguous() and y.is_contiguous() and cu.is_contiguous() and lens.is_contiguous() and table.is_contiguous() and rows.is_contiguous()):
+            raise ValueError("tensors must be contiguous")
         self._project(self.w_q, T, x, self.q)
         self._project(self.w_kv, T, x, self.kv)
         B.latent_append(self.desc, n, T, cu, lens, table, self.kv, self.gain, eps, self.inv_freq, self.q, self.q_rope, rows, self.ws)
@@ -160,7 +176,7 @@ class BlockDecoder(StackDecoder):
         self._one = torch.ones(1, dtype=torch.int32, device=dev)
         self._cu = torch.tensor([0, 1], dtype=torch.int32, device=dev)
         self._lens, self._table = cache.lens[seq:seq + 1], cache.table[seq:seq + 1]
-        dt = {B.F32: torch.float32, B.F16: torch.float16, B.BF16: torch.bfloat16}[desc.out_dtype]
+        dt = _TYPES[desc.out_dtype]
         self.o = torch.empty(desc.H, dtype=dt, device=dev)              # attention output, of the type that the next state is made from
         self.y = torch.empty((self.L, desc.H), dtype=dt, device=dev)
         self.x_moe = torch.empty((self.L, desc.H), dtype=torch.bfloat16, device=dev)

@@ -68,3 +68,53 @@ def test_parts_of_other_sizes_are_refused(edg):
                dict(w_kv=(short[0], short[1].to("meta")))):
         with pytest.raises(ValueError):
             _block(edg, **kw)
+
+
+def _call(edg, **kw):
+    """Arguments of a run of three rows of two sequences"""
+    i = lambda v: torch.tensor(v, dtype=torch.int32)      # noqa: E731
+    return dict(dict(x=torch.zeros((3, H), dtype=torch.bfloat16), y=torch.zeros((3, H)), cu=i([0, 1, 3]), lens=i([5, 9]),
+                     table=torch.zeros((2, 4), dtype=torch.int32), rows=torch.zeros((6, 16, DL + DR), dtype=torch.bfloat16), max_new=2), **kw)
+
+
+@pytest.fixture
+def launched(edg, monkeypatch):
+    """Names of the library's calls, none of which is made"""
+    from paper_2609_18063_b200 import binding
+    names = []
+    for name in ("linear_int4_lora", "latent_append", "latent_attention"):
+        monkeypatch.setattr(binding, name, lambda *a, _n=name, **k: names.append(_n))
+    return names
+
+
+def test_a_run_within_the_bounds_makes_its_calls(edg, launched):
+    _block(edg).run(**_call(edg))
+    assert launched == ["linear_int4_lora"] * 2 + ["latent_append", "latent_attention", "linear_int4_lora"]
+
+
+def test_runs_beyond_the_bounds_launch_nothing(edg, launched):
+    """The block is made for 3 rows of 2 sequences, 2 new ones each, 40 positions."""
+    i = lambda v: torch.tensor(v, dtype=torch.int32)      # noqa: E731
+    b = _block(edg)
+    for T in (4, 8, 64):
+        with pytest.raises(ValueError):
+            b.run(**_call(edg, x=torch.zeros((T, H), dtype=torch.bfloat16), y=torch.zeros((T, H))))
+    for kw in (dict(x=torch.zeros((0, H), dtype=torch.bfloat16), y=torch.zeros((0, H))), dict(cu=i([0])), dict(cu=i([0, 1, 2, 3]), lens=i([5, 9, 9]), table=torch.zeros((3, 4), dtype=torch.int32)),
+               dict(max_new=3), dict(max_new=0), dict(total=41), dict(total=-1),
+               dict(x=torch.zeros((1, H), dtype=torch.bfloat16), y=torch.zeros((1, H)), cu=i([0, 1, 1]))):          # (two new rows of one sequence, one in all)
+        with pytest.raises(ValueError):
+            b.run(**_call(edg, **kw))
+    assert launched == []
+
+
+def test_tensors_that_do_not_fit_launch_nothing(edg, launched):
+    i = lambda v: torch.tensor(v, dtype=torch.int32)      # noqa: E731
+    b = _block(edg)
+    for kw in (dict(x=torch.zeros((3, H))), dict(x=torch.zeros((3, H + 8), dtype=torch.bfloat16)), dict(x=torch.zeros((3, 2 * H), dtype=torch.bfloat16)[:, :H]),
+               dict(y=torch.zeros((3, H), dtype=torch.bfloat16)), dict(y=torch.zeros((2, H))), dict(y=torch.zeros((3, H), device="meta")), dict(y=torch.zeros((3, 2 * H))[:, :H]),
+               dict(cu=torch.tensor([0, 1, 3])), dict(lens=torch.tensor([5, 9])), dict(lens=i([5])), dict(table=torch.zeros((2, 4), dtype=torch.int64)),
+               dict(table=torch.zeros((1, 4), dtype=torch.int32)), dict(table=torch.zeros((2, 5), dtype=torch.int32)), dict(table=torch.zeros(8, dtype=torch.int32)),
+               dict(rows=torch.zeros((5, 16, DL + DR), dtype=torch.bfloat16)), dict(rows=torch.zeros((6, 16, DL + DR))), dict(rows=torch.zeros((6, 16, DL), dtype=torch.bfloat16))):
+        with pytest.raises(ValueError):
+            b.run(**_call(edg, **kw))
+    assert launched == []
