@@ -68,6 +68,8 @@ class LatentCache:
         self.ws = torch.zeros(B.pages_workspace_bytes(self.pool), dtype=torch.uint8, device=device)
 
     def reserve(self, seqs: torch.Tensor, counts: torch.Tensor) -> None:
+        """Grows sequences.  A list that the pool cannot serve, or a sequence that has no room, keeps its lens and is told by status() alone: what
+        appends rows afterwards takes the last positions for the new ones.  Look before it does."""
         B.pages_reserve(self.pool, self.pages, seqs.numel(), seqs, counts, self.ws)
 
     def fork(self, parents: torch.Tensor, children: torch.Tensor) -> None:
@@ -181,18 +183,34 @@ class BlockDecoder(StackDecoder):
         self.y = torch.empty((self.L, desc.H), dtype=dt, device=dev)
         self.x_moe = torch.empty((self.L, desc.H), dtype=torch.bfloat16, device=dev)
         self.x_out = torch.empty((self.L, desc.H), dtype=torch.bfloat16, device=dev)
+        self._most = min(b.bounds[3] for b in blocks)                   # positions that the blocks are made for, and that the cache can hold
+        self._capacity = cache.table.shape[1] * cache.rows.shape[2]
+        self._grow_ws = torch.zeros_like(cache.ws)                      # its status word tells of this request's growth alone
+
+    def _grow(self) -> None:
+        """One more position, or an error with nothing of the token enqueued.  (Whether there is a page is the device's to say: this waits for its
+        answer, and so for the last layer of the token before: some 30 us a token.)"""
+        if self._most < self._capacity and int(self._lens) >= self._most:
+            raise B.EdgError(-4, "BlockDecoder.token")
+        B.pages_reserve(self.cache.pool, self.cache.pages, 1, self._seq, self._one, self._grow_ws)
+        code = B.workspace_status(self._grow_ws)
+        if code != 0:
+            self._grow_ws[:4].zero_()
+            raise B.EdgError(code, "BlockDecoder.token")
 
     def token(self, t: int, x: torch.Tensor, timeout_s: float = 5.0) -> torch.Tensor:
-        """Token t: x device bf16 [H], the first block's input; returns the last block's output (a view that the next token overwrites)."""
+        """Token t: x device bf16 [H], the first block's input; returns the last block's output (a view that the next token overwrites).  Where the
+        pool has no page for the token EdgError -3 is raised, where the sequence is full or the blocks' bound is reached -4: nothing has been
+        changed then, and the token can be asked for again when pages are free."""
         cur, nxt = t % 2, (t + 1) % 2
         mirror, end = self.mirror[cur].numpy(), time.monotonic() + timeout_s
         while (mirror < 0).any():                                       # written by the heads of the token before
             if time.monotonic() > end:
                 raise B.EdgError(-6, "BlockDecoder.token")
+        self._grow()
         self.mirror[nxt].fill_(-1)
         for l in range(self.L):
             self.misses += B.stage_experts_to_slots(self.store, l, mirror[l])[1]
-        self.cache.reserve(self._seq, self._one)
         for l, block in enumerate(self.blocks):
             block.run(x.view(1, -1), self.o, self._cu, self._lens, self._table, self.cache.rows[l])
             B.next_hidden_state(self.desc, x, self.o, self.x_moe[l])
