@@ -172,6 +172,12 @@ class BlockDecoder(StackDecoder):
         super().__init__(desc, store, W_pre)
         if len(blocks) != self.L or cache.rows.shape[0] != self.L:
             raise ValueError("one attention block and one layer of the cache per layer of the store")
+        for b in blocks:
+            d, out = b.desc, b.w_out[0]
+            _refuse((out.N, out.out_dtype) != (desc.H, desc.out_dtype), "a block's output projection writes [H] of the layer's out_dtype")
+            _refuse(tuple(cache.rows.shape[1:]) != (d.n_pages, d.page, d.d_latent + d.d_rope) or cache.table.shape[1] != d.max_pages, "a block's cache is another")
+            _refuse(b.w_uk.device != cache.rows.device, "blocks and cache lie on one device")
+        _refuse(not 0 <= seq < cache.lens.shape[0], "seq is a row of the cache's table")
         self.blocks, self.cache = blocks, cache
         dev = W_pre.device
         self._seq = torch.tensor([seq], dtype=torch.int32, device=dev)
@@ -202,6 +208,7 @@ class BlockDecoder(StackDecoder):
         """Token t: x device bf16 [H], the first block's input; returns the last block's output (a view that the next token overwrites).  Where the
         pool has no page for the token EdgError -3 is raised, where the sequence is full or the blocks' bound is reached -4: nothing has been
         changed then, and the token can be asked for again when pages are free."""
+        _refuse(x.numel() != self.desc.H or x.dtype != torch.bfloat16 or x.device != self.o.device or not x.is_contiguous(), "x is bf16 [H]")
         cur, nxt = t % 2, (t + 1) % 2
         mirror, end = self.mirror[cur].numpy(), time.monotonic() + timeout_s
         while (mirror < 0).any():                                       # written by the heads of the token before

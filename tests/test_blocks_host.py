@@ -118,3 +118,35 @@ def test_tensors_that_do_not_fit_launch_nothing(edg, launched):
         with pytest.raises(ValueError):
             b.run(**_call(edg, **kw))
     assert launched == []
+
+
+@pytest.fixture
+def stack(edg, monkeypatch):
+    """BlockDecoder(blocks, cache, seq) over a stack of one layer that has no store"""
+    from paper_2609_18063_b200 import decoder
+
+    def base(self, desc, store, W_pre, prefetch=True):
+        self.desc, self.store, self.W_pre, self.L = desc, store, W_pre, 1
+    monkeypatch.setattr(decoder.StackDecoder, "__init__", base)
+
+    def make(block=None, cache=None, seq=0, out="f32", **kw):
+        d = edg.make_desc(None, out_dtype=out, **dict(dict(H=H, I=64, E=8, K=2, group=32, rank=8, n_adapters=1, n_slots=4, lora_scale=1.0), **kw))
+        c = decoder.LatentCache(*(cache or (1, 6, 16, DL + DR, 2, 4)), device="cpu")
+        return decoder.BlockDecoder(d, None, torch.zeros(1), [block or _block(edg)], c, seq=seq)
+    return make
+
+
+def test_stacks_whose_parts_do_not_fit_are_refused(edg, stack):
+    assert stack().o.dtype == torch.float32 and stack(seq=1).o.shape == (H,)
+    assert stack(_block(edg, w_out=_projection(edg, H, HEADS * DV, "f16")), out="f16").o.dtype == torch.float16
+    for kw in (dict(out="bf16"), dict(out="f16"), dict(H=2 * H), dict(seq=2), dict(seq=-1), dict(cache=(2, 6, 16, DL + DR, 2, 4)), dict(cache=(1, 5, 16, DL + DR, 2, 4)),
+               dict(cache=(1, 6, 32, DL + DR, 2, 4)), dict(cache=(1, 6, 16, DL, 2, 4)), dict(cache=(1, 6, 16, DL + DR, 2, 5))):
+        with pytest.raises(ValueError):
+            stack(**kw)
+
+
+def test_a_state_that_is_no_state_is_refused_first(edg, stack):
+    dec = stack()
+    for x in (torch.zeros(H), torch.zeros(H - 1, dtype=torch.bfloat16), torch.zeros((2, H), dtype=torch.bfloat16), torch.zeros(2 * H, dtype=torch.bfloat16)[::2]):
+        with pytest.raises(ValueError):
+            dec.token(0, x)
