@@ -36,25 +36,26 @@ __device__ __forceinline__ void raise(int32_t* status, int32_t code) { atomicCAS
 __device__ __forceinline__ int pages_for(int len, int page) { return (int)(((long long)len + page - 1) / page); }
 
 // Exclusive prefix sum over the CTA's kBook threads; total to all.  Two barriers.
-__device__ __forceinline__ int block_scan(int v, int* s_warp, int& total) {
+template <typename I>
+__device__ __forceinline__ I block_scan(I v, I* s_warp, I& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int x = v;
+    I x = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        const I y = __shfl_up_sync(0xFFFFFFFFu, x, o);
         if (lane >= o) x += y;
     }
     if (lane == 31) s_warp[warp] = x;
     __syncthreads();
-    const int w = s_warp[lane];
-    int z = w;
+    const I w = s_warp[lane];
+    I z = w;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xFFFFFFFFu, z, o);
+        const I y = __shfl_up_sync(0xFFFFFFFFu, z, o);
         if (lane >= o) z += y;
     }
     total = __shfl_sync(0xFFFFFFFFu, z, 31);
-    const int before = warp == 0 ? 0 : __shfl_sync(0xFFFFFFFFu, z, warp - 1);
+    const I before = warp == 0 ? 0 : __shfl_sync(0xFFFFFFFFu, z, warp - 1);
     __syncthreads();
     return before + x - v;
 }
@@ -108,6 +109,7 @@ __global__ void __launch_bounds__(128) free_kernel(const edg_page_pool p, int n,
 __global__ void __launch_bounds__(kBook) reserve_kernel(const edg_page_pool p, int n, const int32_t* seqs, const int32_t* counts, int row_bytes,
                                                         const PagesWorkspace w) {
     __shared__ int s_seq[kBook], s_last[kBook], s_first[kBook + 1], s_warp[32];
+    __shared__ long long s_sums[32];
     const int i = threadIdx.x;
     const int seq = i < n ? seqs[i] : -1, cnt = i < n ? counts[i] : 0;
     s_seq[i] = seq;
@@ -135,9 +137,10 @@ __global__ void __launch_bounds__(kBook) reserve_kernel(const edg_page_pool p, i
         for (int j = 0; j < i; ++j) rank += s_last[j] == last;
         copy = rank < p.refs[last] - 1;
     }
-    const int need = ok ? p_new - p_old + (copy ? 1 : 0) : 0;
-    int total;
-    const int first = block_scan(need, s_warp, total);
+    // (1024 sequences of up to 2^31 pages: the sum has 64 bits.  What is beyond the pool counts as one page beyond it.)
+    long long all;
+    const long long before = block_scan<long long>(ok ? p_new - p_old + (copy ? 1 : 0) : 0, s_sums, all);
+    const int total = (int)min(all, p.n_pages + 1ll), first = (int)min(before, p.n_pages + 1ll);
     s_first[i] = first;
     if (i == 0) s_first[kBook] = total;
     // the lowest `total` free pages, in ascending order
