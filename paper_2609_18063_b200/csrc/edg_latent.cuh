@@ -35,8 +35,8 @@ struct LatentSeqs {
 
 // The absorbed form (edg_latent_absorbed.cu) of sequences of up to `most` new rows: scratch, control block included, and the launches.
 size_t absorbed_workspace(const edg_latent_desc& d, int n_seqs, int T, int most);
-int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new, int most, const void* q, const void* q_rope, const void* W_uk,
-                     const void* W_uv, const void* cache, void* y, void* workspace, cudaStream_t st);
+int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new, int64_t total_len, int most, const void* q, const void* q_rope,
+                     const void* W_uk, const void* W_uv, const void* cache, void* y, void* workspace, cudaStream_t st);
 // The expanded form (edg_latent_expanded.cu) of sequences of more new rows than `more_than`: scratch, a control block not among it.
 size_t expanded_workspace(const edg_latent_desc& d, int n_seqs, int T, int64_t total_len);
 int32_t run_expanded(const edg_latent_desc& d, const LatentSeqs& s, int max_new, int64_t total_len, int more_than, const void* q, const void* q_rope,

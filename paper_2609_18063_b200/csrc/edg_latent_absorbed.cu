@@ -52,6 +52,7 @@ struct AbsorbedParams {
     float scale;
     int R, group, groups, max_slots;
     int max_new, most;          // the caller's bound; sequences of up to `most` new rows are taken
+    long long total_len;        // the caller's bound on the sum of lens
 };
 
 namespace {
@@ -79,10 +80,10 @@ __device__ __forceinline__ long long stretch(long long W, int groups) { return q
 
 // Prefix sums over the sequences, and the caller's bounds: 128 threads.
 __device__ __forceinline__ void plan_sequences(const AbsorbedParams& p) {
-        __shared__ long long s_t[128];
+        __shared__ long long s_t[128], s_l[128];
         __shared__ int s_u[128], s_r[128];
         const int tid = threadIdx.x, per = (p.s.n + 127) / 128, i0 = min(tid * per, p.s.n), i1 = min(i0 + per, p.s.n);
-        long long t = 0;
+        long long t = 0, len = 0;
         int u = 0, rows = 0;
         bool ok = tid != 0 || (p.s.cu[0] == 0 && p.s.cu[p.s.n] <= p.s.T);
         for (int i = i0; i < i1; ++i) {
@@ -90,13 +91,17 @@ __device__ __forceinline__ void plan_sequences(const AbsorbedParams& p) {
             t += q.units * unit_length(q);
             u += q.units;
             rows += q.rows > 0 ? q.fresh : 0;
+            len += q.len;
             ok = ok && p.s.cu[i + 1] >= p.s.cu[i] && q.fresh <= p.max_new && q.len >= p.s.lens[i];
         }
-        if (!ok) latent_raise(p.status, EDG_E_RANGE);
+        s_l[tid] = len;
         s_t[tid] = t;
         s_u[tid] = u;
         s_r[tid] = rows;
         __syncthreads();
+        if (tid == 127)                                                  // (the sum sizes nothing here; it is a bound all the same)
+            for (int j = 0; j < 127; ++j) len += s_l[j];
+        if (!ok || len > p.total_len) latent_raise(p.status, EDG_E_RANGE);
         t = 0;
         u = rows = 0;
         for (int j = 0; j < tid; ++j) { t += s_t[j]; u += s_u[j]; rows += s_r[j]; }
@@ -839,8 +844,8 @@ AbsorbedLayout absorbed_layout(const edg_latent_desc& d, int n_seqs, int T, int 
 
 size_t absorbed_workspace(const edg_latent_desc& d, int n_seqs, int T, int most) { return absorbed_layout(d, n_seqs, T, most).bytes; }
 
-int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new, int most, const void* q, const void* q_rope, const void* W_uk, const void* W_uv,
-                     const void* cache, void* y, void* workspace, cudaStream_t st) {
+int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new, int64_t total_len, int most, const void* q, const void* q_rope,
+                     const void* W_uk, const void* W_uv, const void* cache, void* y, void* workspace, cudaStream_t st) {
     const AbsorbedLayout L = absorbed_layout(d, s.n, s.T, most);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     AbsorbedParams p = {};
@@ -872,6 +877,7 @@ int32_t run_absorbed(const edg_latent_desc& d, const LatentSeqs& s, int max_new,
     p.groups = L.groups;
     p.max_slots = L.slots;
     p.max_new = max_new;
+    p.total_len = total_len;
     p.most = most;
     static OncePerDevice once;
     EDG_CUDA_TRY(once([] {

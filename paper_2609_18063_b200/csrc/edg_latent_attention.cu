@@ -66,7 +66,7 @@ extern "C" int32_t latent_attention(const edg_latent_desc* desc, int32_t n_seqs,
     const LatentSeqs s = {cu, lens, table, n_seqs, T, desc->max_pages, __builtin_ctz((unsigned)desc->page), desc->n_pages};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (f.absorbed) {
-        const int32_t e = run_absorbed(*desc, s, max_new, f.most, q, q_rope, W_uk, W_uv, cache, y, workspace, st);
+        const int32_t e = run_absorbed(*desc, s, max_new, total_len, f.most, q, q_rope, W_uk, W_uv, cache, y, workspace, st);
         if (e != EDG_OK) return e;
     }
     if (f.expanded)
