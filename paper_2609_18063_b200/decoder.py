@@ -54,37 +54,6 @@ class StackDecoder:
                                             self.mirror[nxt], Y, self.ws, prefetch=self.prefetch)
 
 
-class LatentCache:
-    """Latent rows of all layers in pages, and which pages a request holds (device state, ``edg.pages_*``)."""
-
-    def __init__(self, layers: int, n_pages: int, page: int, row: int, n_seqs: int, max_pages: int, device="cuda"):
-        """row: d_latent + d_rope values of bf16."""
-        self.rows = torch.zeros((layers, n_pages, page, row), dtype=torch.bfloat16, device=device)
-        self.refs = torch.zeros(n_pages, dtype=torch.int32, device=device)
-        self.table = torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device)
-        self.lens = torch.zeros(n_seqs, dtype=torch.int32, device=device)
-        self.pool = B.make_page_pool(self.refs, self.table, self.lens, page=page)
-        self.pages = B.make_page_cache(self.rows)
-        self.ws = torch.zeros(B.pages_workspace_bytes(self.pool), dtype=torch.uint8, device=device)
-
-    def reserve(self, seqs: torch.Tensor, counts: torch.Tensor) -> None:
-        """Grows sequences.  A list that the pool cannot serve, or a sequence that has no room, keeps its lens and is told by status() alone: what
-        appends rows afterwards takes the last positions for the new ones.  Look before it does."""
-        B.pages_reserve(self.pool, self.pages, seqs.numel(), seqs, counts, self.ws)
-
-    def fork(self, parents: torch.Tensor, children: torch.Tensor) -> None:
-        B.pages_fork(self.pool, parents.numel(), parents, children, self.ws)
-
-    def free(self, seqs: torch.Tensor) -> None:
-        B.pages_free(self.pool, seqs.numel(), seqs, self.ws)
-
-    def compact(self) -> None:
-        B.pages_compact(self.pool, self.pages, self.ws)
-
-    def status(self) -> int:
-        return B.workspace_status(self.ws)
-
-
 _TYPES = {B.F32: torch.float32, B.F16: torch.float16, B.BF16: torch.bfloat16}
 
 
@@ -96,6 +65,45 @@ def _refuse(bad: bool, what: str) -> None:
 def _is(t, shape, dtype, device) -> bool:
     """Whether t is a tensor like that (an address says nothing about itself: taken as given)."""
     return not isinstance(t, torch.Tensor) or (tuple(t.shape) == tuple(shape) and t.dtype == dtype and t.device == device)
+
+
+class LatentCache:
+    """Latent rows of all layers in pages, and which pages a request holds (device state, ``edg.pages_*``).  Lists are int32 tensors on the cache's
+    device, those of one call of one length; anything else is a ValueError."""
+
+    def __init__(self, layers: int, n_pages: int, page: int, row: int, n_seqs: int, max_pages: int, device="cuda"):
+        """row: d_latent + d_rope values of bf16."""
+        self.rows = torch.zeros((layers, n_pages, page, row), dtype=torch.bfloat16, device=device)
+        self.refs = torch.zeros(n_pages, dtype=torch.int32, device=device)
+        self.table = torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device)
+        self.lens = torch.zeros(n_seqs, dtype=torch.int32, device=device)
+        self.pool = B.make_page_pool(self.refs, self.table, self.lens, page=page)
+        self.pages = B.make_page_cache(self.rows)
+        self.ws = torch.zeros(B.pages_workspace_bytes(self.pool), dtype=torch.uint8, device=device)
+
+    def _lists(self, *lists: torch.Tensor) -> None:
+        for v in lists:
+            _refuse(v.dtype != torch.int32 or v.device != self.lens.device or v.numel() != lists[0].numel(), "lists are int32 [n] on the cache's device")
+
+    def reserve(self, seqs: torch.Tensor, counts: torch.Tensor) -> None:
+        """Grows sequences.  A list that the pool cannot serve, or a sequence that has no room, keeps its lens and is told by status() alone: what
+        appends rows afterwards takes the last positions for the new ones.  Look before it does."""
+        self._lists(seqs, counts)
+        B.pages_reserve(self.pool, self.pages, seqs.numel(), seqs, counts, self.ws)
+
+    def fork(self, parents: torch.Tensor, children: torch.Tensor) -> None:
+        self._lists(parents, children)
+        B.pages_fork(self.pool, parents.numel(), parents, children, self.ws)
+
+    def free(self, seqs: torch.Tensor) -> None:
+        self._lists(seqs)
+        B.pages_free(self.pool, seqs.numel(), seqs, self.ws)
+
+    def compact(self) -> None:
+        B.pages_compact(self.pool, self.pages, self.ws)
+
+    def status(self) -> int:
+        return B.workspace_status(self.ws)
 
 
 class LatentBlock:

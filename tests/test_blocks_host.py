@@ -150,3 +150,25 @@ def test_a_state_that_is_no_state_is_refused_first(edg, stack):
     for x in (torch.zeros(H), torch.zeros(H - 1, dtype=torch.bfloat16), torch.zeros((2, H), dtype=torch.bfloat16), torch.zeros(2 * H, dtype=torch.bfloat16)[::2]):
         with pytest.raises(ValueError):
             dec.token(0, x)
+
+
+def test_lists_that_are_no_lists_are_refused(edg, monkeypatch):
+    """Of another type, on another device than the cache, or shorter than the one beside them: the kernels would read behind them."""
+    from paper_2609_18063_b200 import binding, decoder
+    names = []
+    for name in ("pages_reserve", "pages_fork", "pages_free"):
+        monkeypatch.setattr(binding, name, lambda *a, _n=name: names.append(_n))
+    c = decoder.LatentCache(1, 6, 16, DL + DR, 2, 4, device="cpu")
+    i = lambda v, **kw: torch.tensor(v, dtype=torch.int32, **kw)      # noqa: E731
+    for bad in (torch.tensor([0, 1]), i([0, 1]).to("meta"), torch.tensor([0.0, 1.0])):
+        for call in (lambda: c.reserve(bad, i([1, 1])), lambda: c.reserve(i([0, 1]), bad), lambda: c.fork(bad, i([1, 1])), lambda: c.fork(i([0, 0]), bad), lambda: c.free(bad)):
+            with pytest.raises(ValueError):
+                call()
+    for call in (lambda: c.reserve(i([0, 1]), i([1])), lambda: c.fork(i([0]), i([0, 1]))):
+        with pytest.raises(ValueError):
+            call()
+    assert names == []
+    c.reserve(i([0, 1]), i([1, 5]))
+    c.fork(i([0]), i([1]))
+    c.free(i([0]))
+    assert names == ["pages_reserve", "pages_fork", "pages_free"]
