@@ -425,6 +425,8 @@ def make_page_pool(refs, table, lens, *, page) -> PagePool:
     """The struct only carries addresses (int32 tensors refs [n_pages], table [n_seqs][max_pages], lens [n_seqs]): the caller keeps them alive."""
     if table.shape[0] != lens.shape[0]:
         raise ValueError("table and lens disagree about the number of sequences")
+    if any(str(t.dtype).rsplit(".", 1)[-1] != "int32" for t in (refs, table, lens)):
+        raise ValueError("refs, table and lens are int32")
     return PagePool(refs.shape[0], int(page), table.shape[0], table.shape[1], _ptr(refs), _ptr(table), _ptr(lens))
 
 
