@@ -436,8 +436,8 @@ int32_t edg_linear_workspace_bytes(const edg_linear_desc* desc, int32_t T, size_
 
 /* record dev; x dev bf16 [T][ldx], each row 16-byte aligned; A dev bf16 [rank][Kd] and B dev bf16 [N][rank], 16-byte aligned (read only
  * with rank > 0); y dev [T][ldy] of out_dtype, aligned to its type (columns N.. of a row are not touched); workspace 256-byte aligned, needs no
- * initialisation; calls that share one must be ordered on the device.  1 <= T <= 65535; made for batched decode: the weights are
- * read once for every 64 tokens.  Codes enter the products exactly, activations as fp16 beside a power of two per token (2^-34 of the
+ * initialisation; calls that share one must be ordered on the device.  1 <= T <= 65535; made for batched decode: every 16 tokens, or 8
+ * where that is less work, go through the weights once more, so the time of longer calls grows with T.  Codes enter the products exactly, activations as fp16 beside a power of two per token (2^-34 of the
  * largest one is lost), sums are fp32. */
 int32_t linear_int4_lora(const edg_linear_desc* desc, const void* record, int32_t T, const void* x, const void* A, const void* B,
                          void* y, void* workspace, size_t workspace_bytes, void* stream);
@@ -484,7 +484,8 @@ int32_t edg_pages_fork(const edg_page_pool* pool, int32_t n, const int32_t* pare
  * page that is partly filled and shared is replaced by a copy of its filled rows first (in every layer of `cache`), so that what is
  * written behind them reaches this sequence alone; of all holders that grow, the last in the list keeps the page if no
  * other holds it.  New pages are the lowest-numbered free ones, given out in the order of the list: first the copy, then the
- * others.  Where the pool has too few free pages for the whole list, nothing is changed and EDG_E_SLOTS is raised. */
+ * others.  Where the pool has too few free pages for the whole list, nothing is changed and EDG_E_SLOTS is raised.  A sequence that did not
+ * grow keeps its length: whoever then appends rows to it writes over its last ones, so the status word is read before. */
 int32_t edg_pages_reserve(const edg_page_pool* pool, const edg_page_cache* cache, int32_t n, const int32_t* seqs, const int32_t* counts,
                           void* workspace, size_t workspace_bytes, void* stream);
 

@@ -19,9 +19,9 @@
 // Rounded to bf16, by 2^-8 of a value at most: q_lat and p, which are operands beside the cache's bf16 (l sums p as it was rounded).  O, m and l
 // are fp32 throughout; the latent sums go into the last product as two bf16 parts, 16 bits in all.
 //
-// Of the cache, 512 + 64 columns: 8 sequences of 65,536 positions, 128 heads (R = 64, two CTAs side by side) 219 us -- 3,000 clocks a tile, of which the
+// Of the cache, 512 + 64 columns: 8 sequences of 65,536 positions, 128 heads (R = 64, two CTAs side by side) 219 to 252 us, by the box -- 3,000 clocks a tile, of which the
 // products take 2,100 and shared memory 2,500 (36 products of 37 clocks for S, whose M = 64 is half of what the tensor cores take; 16 of 49
-// for O; the copies of 74 KB); 32 sequences of 1 to 8,191, 32 heads (R = 32) 52 us -- the tiles by themselves come at 6.5 TB/s (16 us), the
+// for O; the copies of 74 KB); 32 sequences of 1 to 8,191, 32 heads (R = 32) 52 to 54 us -- the tiles by themselves come at 6.5 TB/s (16 us), the
 // rest is absorb_kernel (9), the first tile (6) and combine_kernel (15, of W_uv and the code's first fetch more than of the pieces: half as
 // many rows to a CTA took as long).
 #include "edg_latent.cuh"

@@ -17,9 +17,9 @@
 // would not hold its range.  Maxima, sums and O are fp32.  Of a standard normal batch the outputs before their own rounding are 0.2% off in the
 // mean square.
 //
-// 4,430 new rows of three sequences of 7,103 positions, 32 heads of 128 + 64 / 128, 512 latent columns: expand_kernel 62 us (62 GFLOP: 1.0
-// PFLOP/s; its limits are the weights, which every CTA reads from L2, and its two rounds of CTAs), prompt_kernel 182 us (185 GFLOP of rows that
-// see one another: 1.0 PFLOP/s).  A pair of tiles takes 3,900 clocks, with products under way for 3,260 (2,600 by their
+// 4,430 new rows of three sequences of 7,103 positions, 32 heads of 128 + 64 / 128, 512 latent columns: 227 to 275 us, by the box; on one that takes
+// 250, expand_kernel 62 to 66 (62 GFLOP: 1.0 PFLOP/s; its limits are the weights, which every CTA reads from L2, and its two rounds of CTAs),
+// prompt_kernel 182 to 186 (185 GFLOP of rows that see one another: 1.0 PFLOP/s).  A pair of tiles takes 3,900 clocks, with products under way for 3,260 (2,600 by their
 // operations); S of a tile, its softmax (2,050) and P V follow one another, since neither tensor memory has room for a third S nor shared
 // memory for P.
 #include "edg_latent.cuh"
@@ -56,6 +56,8 @@ __device__ __forceinline__ XSeq xsequence(const ExpandedParams& p, int i) {
     q.tiles = mine ? (q.len + 127) >> 7 : 0;
     return q;
 }
+
+constexpr int kSms = 148;                   // what a launch is sized by
 
 // prefix sums over the sequences, and the caller's bounds
 __global__ void __launch_bounds__(256) prompt_plan_kernel(const __grid_constant__ ExpandedParams p) {
@@ -289,7 +291,6 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
 
 // ---------------------------------------------------------------- attention
 
-constexpr int kSms = 148;
 constexpr int kPThreads = 640;              // warp 0 takes work and loads, 1 issues products, 4-11 and 12-19 are the softmax of a tile of rows each
 constexpr int kPRing = 8;
 constexpr uint32_t kPQ = 0, kPRingAt = 6 * kChunk, kPBars = kPRingAt + kPRing * kChunk, kPItems = kPBars + 320, kPMax = kPItems + 64,
@@ -730,7 +731,7 @@ int32_t run_expanded(const edg_latent_desc& d, const LatentSeqs& s, int max_new,
     const int64_t tiles = L.rows / 128;
     int64_t least = 0;
     for (int x = 1; x <= d.heads; ++x) {
-        const int64_t cost = (tiles * x + 147) / 148 * ((d.heads + x - 1) / x + 1);
+        const int64_t cost = (tiles * x + kSms - 1) / kSms * ((d.heads + x - 1) / x + 1);
         if (x == 1 || cost < least) { least = cost; p.splits = x; }
     }
     static OncePerDevice once;

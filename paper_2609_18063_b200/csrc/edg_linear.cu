@@ -17,7 +17,8 @@
 // the GPU.  Partial sums meet in shared memory, in a fixed order.
 //
 // 64,001 x 2,048 codes (74 MB with their scales): 1 token 18.1 us (4.1 TB/s), 8 20.5, 16 31, 64 97; 6,144 x 2,048 with an adapter of 16:
-// 1 token 7.9, 64 23.5; 1,024 x 1,024, 1 token: 6.7 (two launches and two waits for memory).  From 16 tokens on the products bound it: every 8
+// 1 token 7.9, 64 23.5, 4,096 623 (ten times what its operations take); 1,024 x 1,024, 1 token: 6.7 (two launches and two waits for memory).
+// From 16 tokens on the products bound it: a slice of the grid for every 8 or 16 tokens takes the codes apart again, and every 8
 // tokens more cost 11 us of the first, 25 clocks a product and quarter of an SM.
 #include <cooperative_groups.h>
 #include <string.h>
