@@ -511,7 +511,8 @@ int32_t edg_pages_copy(const edg_page_cache* dst, const edg_page_cache* src, int
  *   absorbed   q_lat = W_uk[h]^T q_nope, o_lat = sum_j p_j c_j, y = W_uv[h] o_lat: reads every cache row once for all heads (decoding)
  *   expanded   keys and values of every head are written out once, then plain attention over them (prompts)
  * Both take bf16 operands with fp32 sums and softmax; q_lat, o_lat (as two bf16 parts) and the weights softmax(s) enter products as bf16 in
- * the absorbed form, the expanded keys and values and the weights in the other: half a bf16 step each, as y itself.  EDG_LATENT_AUTO takes the
+ * the absorbed form, the expanded keys in the other: half a bf16 step each, as y itself in bf16 and more than y itself in fp16.  The other's values and weights are fp16 (half a step: 2^-11) in
+ * each tile of 128 positions where the magnitudes of its rows and of W_uv show that fp16 holds the values, and bf16 elsewhere.  EDG_LATENT_AUTO takes the
  * form of a sequence by its new rows and by the bounds that a call gives; the results of the two differ by those roundings. */
 #define EDG_LATENT_AUTO     0
 #define EDG_LATENT_ABSORBED 1

@@ -13,13 +13,15 @@
 // after that takes what S has read).  Positions behind a sequence's end are padded to 128; their values are written as zeros, their scores
 // never looked at.
 //
-// K, V and P are rounded to bf16, by 2^-8 of a value at most: the operands of a product have one type, the cache's is bf16, and fp16
-// would not hold its range.  Maxima, sums and O are fp32.  Of a standard normal batch the outputs before their own rounding are 0.2% off in the
-// mean square.
+// K is rounded to bf16, by 2^-8 of a value at most: the operands of a product have one type, and the queries' is bf16.  V and P are rounded to fp16, by
+// 2^-11, wherever that holds their range: |V| is at most d_l times the largest of a row of W_uv times the largest of a cache row, so the exponents of
+// these tell, for a tile of positions, whether V stays below 2^15 and whether it is large enough for what fp16 cuts off at 2^-25 not to count.  In
+// other tiles both are bf16, which holds any range.  Maxima, sums and O are fp32.  Of a standard normal batch the outputs before their own rounding are
+// 0.1% off in the mean square (0.2% with V and P in bf16).
 //
-// 4,430 new rows of three sequences of 7,103 positions, 32 heads of 128 + 64 / 128, 512 latent columns: 227 to 275 us, by the box; on one that takes
-// 250, expand_kernel 62 to 66 (62 GFLOP: 1.0 PFLOP/s; its limits are the weights, which every CTA reads from L2, and its two rounds of CTAs),
-// prompt_kernel 182 to 186 (185 GFLOP of rows that see one another: 1.0 PFLOP/s).  A pair of tiles takes 3,900 clocks, with products under way for 3,260 (2,600 by their
+// 4,430 new rows of three sequences of 7,103 positions, 32 heads of 128 + 64 / 128, 512 latent columns: 232 to 282 us, by the box; under a
+// profiler the plan and the look through W_uv 5, expand_kernel 64 to 67 (62 GFLOP: 1.0 PFLOP/s; its limits are the weights, which every CTA reads from
+// L2, and its two rounds of CTAs), prompt_kernel 190 (185 GFLOP of rows that see one another: 1.0 PFLOP/s).  A pair of tiles takes 3,900 clocks, with products under way for 3,260 (2,600 by their
 // operations); S of a tile, its softmax (2,050) and P V follow one another, since neither tensor memory has room for a third S nor shared
 // memory for P.
 #include "edg_latent.cuh"
@@ -33,6 +35,9 @@ struct ExpandedParams {
     uint16_t *K, *V, *Rp;       // [heads][rows][dn], [heads][rows][dv], [rows][64] (rotated part and zeros)
     int32_t *q_pre, *kv_pre;    // [n + 1] pairs of row tiles before a sequence; tiles of 128 positions before it
     int32_t* next;              // the next pair of row tiles (of a head) to be taken
+    const uint16_t* W_uv;
+    int32_t* w_range;           // [kScan] exponents of the largest values of rows of W_uv: most << 16 | least
+    int32_t* halves;            // [rows / 128] whether V of a tile of positions, and P beside it, is fp16
     void* y;
     int32_t* status;
     int heads, dn, dr, dv, dl, out_dtype;
@@ -59,9 +64,49 @@ __device__ __forceinline__ XSeq xsequence(const ExpandedParams& p, int i) {
 
 constexpr int kSms = 148;                   // what a launch is sized by
 
-// prefix sums over the sequences, and the caller's bounds
+// Biased exponents of the largest magnitudes of rows (of cache or W_uv): the most and the least of them, rows of zeros aside.
+struct Exponents {
+    unsigned most = 0, least = 511;
+    __device__ __forceinline__ void row(unsigned magnitude) {            // (bits of a bf16 without its sign)
+        if (magnitude == 0) return;
+        most = max(most, magnitude >> 7);
+        least = min(least, magnitude >> 7);
+    }
+    __device__ __forceinline__ void join(unsigned packed) { most = max(most, packed >> 16); least = min(least, packed & 0xFFFFu); }
+    __device__ __forceinline__ unsigned packed() const { return most << 16 | least; }
+};
+// V is a sum of d_l <= 2^9 products of values below 2^(e - 126): below 2^15 where the two exponents add up to 258 at most.  Where they add up to 246 at least,
+// V of rows without outliers is some 2^-7 and more, of which fp16 cuts off 2^-25: a value has to be 2^-9 of that before bf16 would hold it better.
+__device__ __forceinline__ bool fits_half(const Exponents& w, const Exponents& c) { return w.most + c.most <= 258 && w.least + c.least >= 246; }
+
+// CTAs of the plan that look through W_uv
+constexpr int kScan = 128;
+__device__ __forceinline__ void scan_values(const ExpandedParams& p, int cta) {
+    __shared__ unsigned s_range[8];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = p.heads * p.dv;
+    Exponents e;
+#pragma unroll 4
+    for (int r = cta * 8 + warp; r < rows; r += kScan * 8) {
+        const uint16_t* w = p.W_uv + (size_t)r * p.dl + lane * 8;
+        uint32_t m = 0;
+        if (lane * 8 < p.dl) m = bf16_magnitudes(m, __ldg(reinterpret_cast<const uint4*>(w)));
+        if (256 + lane * 8 < p.dl) m = bf16_magnitudes(m, __ldg(reinterpret_cast<const uint4*>(w + 256)));
+        e.row(__reduce_max_sync(0xFFFFFFFFu, max(m & 0xFFFFu, m >> 16)));
+    }
+    if (lane == 0) s_range[warp] = e.packed();
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int i = 1; i < 8; ++i) e.join(s_range[i]);
+    p.w_range[cta] = (int32_t)e.packed();
+}
+
+// prefix sums over the sequences, and the caller's bounds; the other CTAs look through W_uv meanwhile
 __global__ void __launch_bounds__(256) prompt_plan_kernel(const __grid_constant__ ExpandedParams p) {
     pdl_launch_dependents();
+    if (blockIdx.x > 0) {
+        scan_values(p, blockIdx.x - 1);
+        return;
+    }
     if (threadIdx.x == 0) *p.next = 0;
     __shared__ int s_q[8], s_k[8];
     __shared__ long long s_l[8], s_f[8];
@@ -147,6 +192,7 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *s_tmem;
+    __shared__ unsigned s_rows[4], s_weights[4];                         // exponents by warp: of this tile's cache rows, of W_uv
     const int tile = blockIdx.x, split = blockIdx.y;
     const int h0 = (int)((int64_t)p.heads * split / p.splits), h1 = (int)((int64_t)p.heads * (split + 1) / p.splits);
     const bool there = tile < p.kv_pre[p.s.n] && (tile + 1) * 128 <= p.rows;
@@ -238,6 +284,20 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
             __syncwarp();
             if (lane == 0) mbar_arrive(a_full);
             const bool finite = !bf16_not_finite(most);
+            Exponents rows, weights;
+            rows.row(held && finite ? max(most & 0xFFFFu, most >> 16) : 0u);
+            weights.join((unsigned)p.w_range[tid - 128]);
+            static_assert(kScan == 128, "one to a thread");
+            rows.most = __reduce_max_sync(0xFFFFFFFFu, rows.most);
+            rows.least = __reduce_min_sync(0xFFFFFFFFu, rows.least);
+            weights.most = __reduce_max_sync(0xFFFFFFFFu, weights.most);
+            weights.least = __reduce_min_sync(0xFFFFFFFFu, weights.least);
+            if (lane == 0) { s_rows[wq] = rows.packed(); s_weights[wq] = weights.packed(); }
+            barrier_sync(1, 128);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { rows.join(s_rows[i]); weights.join(s_weights[i]); }
+            const bool in_half = fits_half(weights, rows);
+            if (split == 0 && tid == 128) p.halves[tile] = in_half;
             if (split == 0) {                                            // the rotated part of this thread's row
                 uint4* out = reinterpret_cast<uint4*>(p.Rp + ((size_t)tile * 128 + row) * 64);
                 const int at = pos0 + row;
@@ -257,17 +317,21 @@ __global__ void __launch_bounds__(kXThreads, 1) expand_kernel(const __grid_const
                     uint8_t* stage = smem + kXOut + wq * 8192;
                     role_wait(&d_full[j & 1], (uint32_t)(j >> 1) & 1, p.status);
                     tc_fence_after();
+                    auto round = [&](auto pair) {
 #pragma unroll 2
-                    for (int c = 0; c < n; c += 16) {
-                        uint32_t v[16];
-                        tmem_ld(tmem + lanes + (j & 1) * 128 + c, v);
-                        uint32_t o[8];
+                        for (int c = 0; c < n; c += 16) {
+                            uint32_t v[16];
+                            tmem_ld(tmem + lanes + (j & 1) * 128 + c, v);
+                            uint32_t o[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) o[i] = keep ? bf16_pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])) : 0u;
+                            for (int i = 0; i < 8; ++i) o[i] = keep ? pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])) : 0u;
 #pragma unroll
-                        for (int x = 0; x < 2; ++x)
-                            *reinterpret_cast<uint4*>(stage + lane * 256 + (((c / 8 + x) ^ (lane & 7)) * 16)) = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
-                    }
+                            for (int x = 0; x < 2; ++x)
+                                *reinterpret_cast<uint4*>(stage + lane * 256 + (((c / 8 + x) ^ (lane & 7)) * 16)) = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+                        }
+                    };
+                    if (kv == 1 && in_half) round([](float a, float b) { return half_pair(a, b); });
+                    else round([](float a, float b) { return bf16_pair(a, b); });
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&d_empty[j & 1]);
@@ -296,7 +360,7 @@ constexpr int kPRing = 8;
 constexpr uint32_t kPQ = 0, kPRingAt = 6 * kChunk, kPBars = kPRingAt + kPRing * kChunk, kPItems = kPBars + 320, kPMax = kPItems + 64,
                    kPBytes = kPMax + 2048;
 
-// Two tiles of 128 new rows of one head, and what they see.  h < 0: there is no more.
+// Two tiles of 128 new rows of one head, and what they see.  h < 0: there is no more.  (Read until the item is done.)
 struct alignas(16) Item { int h, kv0, pos0, token, rows, n[2], unused; };
 
 __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_constant__ ExpandedParams p, const __grid_constant__ CUtensorMap qn_map,
@@ -343,14 +407,6 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
     // A CTA takes pairs of tiles one after another: the next one's queries and keys are loaded, and its first tile begun, while the second tile
     // of this one is finished (a CTA a pair stood for 5,000 clocks before its first S and 5,000 after its last, of some 75,000).
     RingAt it;
-    auto take_item = [&](Item& x) {
-        role_wait(&item_full[it.slot], it.phase, p.status);
-        x = s_item[it.slot];
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&item_empty[it.slot]);
-        it.next(2);
-        return x.h >= 0;
-    };
     {
         const int nkc = (p.dn + 63) / 64, nvc = (p.dv + 63) / 64;        // chunks of keys (and one of rotated parts), of values
         if (warp >= 4) {
@@ -362,12 +418,20 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
             float* my_max = s_max + (i * 2 + half) * 128 + wq * 32 + lane;
             float* their_max = s_max + (i * 2 + 1 - half) * 128 + wq * 32 + lane;
             uint32_t done = 0;                                           // tiles, of all items
-            Item x;
-            while (take_item(x)) {
-            const int pos = x.pos0 + row, mine = i == 0 ? x.n[0] : x.n[1];        // positions 0 .. pos are seen
-            uint16_t* const out = row < x.rows ? static_cast<uint16_t*>(p.y) + ((size_t)(x.token + row) * p.heads + x.h) * p.dv : nullptr;
+            // (An item's place is given back when it is done: what of it is needed at its end takes no registers in between.)
+            while (true) {
+            role_wait(&item_full[it.slot], it.phase, p.status);
+            const Item& x = s_item[it.slot];
+            if (x.h < 0) break;
+            auto item_done = [&]() {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&item_empty[it.slot]);
+                it.next(2);
+            };
+            const int pos = x.pos0 + row, mine = x.n[i];                 // positions 0 .. pos are seen
             float m = -INFINITY, l = 0.f;                                // (l: of this thread's columns)
             for (int t = 0; t < mine; ++t, ++done) {
+                const int in_half = __ldcg(p.halves + (x.kv0 >> 7) + t);        // (there long before it is used)
                 role_wait(&s_full[i], done & 1, p.status);
                 tc_fence_after();
                 const int seen = pos + 1 - t * 128 - half * 64;          // of these columns
@@ -414,24 +478,28 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                 }
                 const float mm = m == -INFINITY ? 0.f : -m;
                 float2 sum = make_float2(0.f, 0.f);
+                auto weights = [&](auto pair) {
 #pragma unroll
-                for (int c = 0; c < 64; c += 32) {
-                    uint32_t o[16];
+                    for (int c = 0; c < 64; c += 32) {
+                        uint32_t o[16];
 #pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        const float x = exp2_approx(fmaf(__uint_as_float(v[c + j]), k2, mm)), y = exp2_approx(fmaf(__uint_as_float(v[c + j + 1]), k2, mm));
-                        sum.x += x;
-                        sum.y += y;
-                        o[j / 2] = bf16_pair(x, y);
+                        for (int j = 0; j < 32; j += 2) {
+                            const float x = exp2_approx(fmaf(__uint_as_float(v[c + j]), k2, mm)), y = exp2_approx(fmaf(__uint_as_float(v[c + j + 1]), k2, mm));
+                            sum.x += x;
+                            sum.y += y;
+                            o[j / 2] = pair(x, y);
+                        }
+                        tmem_st(st + half * 32 + c / 2, o);              // (over the scores of the first half, which all have read: the barrier above)
+                        if (c == 0) {                                    // (half of P V can begin)
+                            tmem_st_wait();
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&p_half[i]);
+                        }
                     }
-                    tmem_st(st + half * 32 + c / 2, o);                  // (over the scores of the first half, which all have read: the barrier above)
-                    if (c == 0) {                                        // (half of P V can begin)
-                        tmem_st_wait();
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&p_half[i]);
-                    }
-                }
+                };
+                if (in_half != 0) weights([](float a, float b) { return half_pair(a, b); });
+                else weights([](float a, float b) { return bf16_pair(a, b); });
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
@@ -440,12 +508,14 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
             }
             // ---- out
             // (straight from the registers, a sector at a time: by way of the queries' place, for whole lines, the next queries came 6,000 clocks later)
+            uint16_t* const out = row < x.rows ? static_cast<uint16_t*>(p.y) + ((size_t)(x.token + row) * p.heads + x.h) * p.dv : nullptr;
             if (mine == 0) {                                             // rows that see nothing, or none
                 if (out != nullptr)
                     for (int c = half * 16; c < p.dv; c += 32) {
                         *reinterpret_cast<uint4*>(out + c) = make_uint4(0, 0, 0, 0);
                         *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(0, 0, 0, 0);
                     }
+                item_done();
                 continue;
             }
             // (A sum goes to the place of the other half's maximum, whose one reader is this thread: behind the last tile nothing tells that the
@@ -475,6 +545,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                 __syncwarp();
             }
             tc_fence_before();
+            item_done();
             }
         } else {
             if (warp == 0) {
@@ -570,7 +641,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
             // ========================================= products, by one thread: for each tile of rows O += P V of a tile of positions, then S of the
             // next.  (What it does between two products is time in which the tensor cores wait: they hold two or three products of 65 clocks.)
             if (elected()) {
-                const uint32_t id_s = idesc_bf16(128, 128), id_o = idesc_bf16(128, p.dv, false, true);
+                const uint32_t id_s = idesc_bf16(128, 128), id_any = idesc_bf16(128, p.dv, false, true);
                 const uint32_t dq = desc_lo(sb + kPQ), dk = desc_lo(sb + kPRingAt), dv = desc_lo(sb + kPRingAt, kChunk);
                 const int rks = p.dr / 16;
                 RingAt f;                                                // the next group (keys or values) to wait for
@@ -602,6 +673,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                     role_wait(&item_full[it.slot], it.phase, p.status);
                     const int n[2] = {s_item[it.slot].n[0], s_item[it.slot].n[1]};
                     const bool end = s_item[it.slot].h < 0;
+                    const int first = s_item[it.slot].kv0 >> 7;
                     mbar_arrive(&item_empty[it.slot]);
                     it.next(2);
                     if (end) break;
@@ -621,6 +693,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                         release();
                     }
                     for (int t = 0; t < nt; ++t) {
+                        const uint32_t types = __ldcg(p.halves + first + t) != 0 ? kIdescTypes : 0u, id_o = id_any - types;
                         const int v = take(nvc);
                         const RingAt fv = f;                             // the values, and the next keys
                         f.next(kPRing);
@@ -651,7 +724,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                                 } else {
                                     role_wait(&p_full[i], tiles[i]++ & 1, p.status);
                                     tc_fence_after();
-                                    const uint32_t id0 = idesc_bf16(128, 64, false, true), id1 = idesc_bf16(128, p.dv - 64, false, true);
+                                    const uint32_t id0 = idesc_bf16(128, 64, false, true) - types, id1 = idesc_bf16(128, p.dv - 64, false, true) - types;
 #pragma unroll
                                     for (int s = 0; s < 8; ++s) {
                                         umma_ts(o, pt + s * 8, b + ((s * 2048) >> 4), id0, t + s > 0);
@@ -681,7 +754,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
     if (warp == 1) tmem_free(tmem, 512);
 }
 
-struct ExpandedLayout { int rows; size_t q_pre, kv_pre, next, K, V, Rp, bytes; };
+struct ExpandedLayout { int rows; size_t q_pre, kv_pre, next, range, halves, K, V, Rp, bytes; };
 
 ExpandedLayout expanded_layout(const edg_latent_desc& d, int n_seqs, int T, int64_t total_len) {
     ExpandedLayout L;
@@ -690,7 +763,9 @@ ExpandedLayout expanded_layout(const edg_latent_desc& d, int n_seqs, int T, int6
     L.q_pre = 0;
     L.kv_pre = round_up(((size_t)n_seqs + 1) * 4, 256);
     L.next = 2 * L.kv_pre;
-    L.Rp = L.next + 256;
+    L.range = L.next + 256;
+    L.halves = L.range + kScan * 4;
+    L.Rp = round_up(L.halves + (size_t)rows / 128 * 4, 256);
     L.K = L.Rp + (size_t)rows * 128;
     L.V = round_up(L.K + (size_t)rows * d.heads * d.d_nope * 2, 256);
     L.bytes = round_up(L.V + (size_t)rows * d.heads * d.d_v * 2, 256);
@@ -714,6 +789,9 @@ int32_t run_expanded(const edg_latent_desc& d, const LatentSeqs& s, int max_new,
     p.q_pre = reinterpret_cast<int32_t*>(ws + L.q_pre);
     p.kv_pre = reinterpret_cast<int32_t*>(ws + L.kv_pre);
     p.next = reinterpret_cast<int32_t*>(ws + L.next);
+    p.W_uv = static_cast<const uint16_t*>(W_uv);
+    p.w_range = reinterpret_cast<int32_t*>(ws + L.range);
+    p.halves = reinterpret_cast<int32_t*>(ws + L.halves);
     p.y = y;
     p.status = status;
     p.heads = d.heads;
@@ -778,7 +856,7 @@ int32_t run_expanded(const edg_latent_desc& d, const LatentSeqs& s, int max_new,
         const uint64_t dims[2] = {64, rows}, stride = 64;
         EDG_CUDA_TRY(make_map(&r_map, p.Rp, 2, dims, &stride, rows128));
     }
-    prompt_plan_kernel<<<1, 256, 0, st>>>(p);
+    prompt_plan_kernel<<<1 + kScan, 256, 0, st>>>(p);
     EDG_CUDA_TRY(cudaGetLastError());
     EDG_CUDA_TRY(launch_pdl(expand_kernel, dim3((unsigned)tiles, p.splits), kXThreads, kXBytes, st, p, c_map, uk_map, uv_map));
     const int64_t pairs = (int64_t)d.heads * (s.T / 256 + (s.n < s.T ? s.n : s.T));       // at most

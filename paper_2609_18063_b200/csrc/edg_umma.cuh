@@ -19,6 +19,7 @@ __device__ __forceinline__ uint32_t desc_lo(uint32_t saddr, uint32_t chunk = 16)
 __host__ __device__ constexpr uint32_t idesc_bf16(int m, int n, bool a_mn = false, bool b_mn = false) {
     return (1u << 4) | (1u << 7) | (1u << 10) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
+constexpr uint32_t kIdescTypes = (1u << 7) | (1u << 10);                       // without these bits both operands are fp16
 __device__ __forceinline__ void umma_ss(uint32_t tmem_d, uint32_t da, uint32_t db, uint32_t idesc, bool accumulate) {
     asm volatile("{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %4, 0;\nmov.b64 a, {%1, %5};\nmov.b64 b, {%2, %5};\n"
                  "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}"
@@ -138,6 +139,12 @@ __device__ __forceinline__ bool bf16_not_finite(uint32_t m) { return (m & 0xFFFF
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+}
+// two fp32 -> packed fp16, a in the low half
+__device__ __forceinline__ uint32_t half_pair(float a, float b) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
     return r;
 }
 
