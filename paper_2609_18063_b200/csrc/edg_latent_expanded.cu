@@ -476,7 +476,8 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                     }
                     tmem_st_wait();
                 }
-                const float mm = m == -INFINITY ? 0.f : -m;
+                // (2^7 more than 2^(s - m), at most 2^15: what fp16 cuts off is then 2^-32 of the largest weight, and a million of the smallest count)
+                const float mm = m == -INFINITY ? 0.f : 7.f - m;
                 float2 sum = make_float2(0.f, 0.f);
                 auto weights = [&](auto pair) {
 #pragma unroll
