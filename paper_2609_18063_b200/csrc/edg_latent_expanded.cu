@@ -476,8 +476,9 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_kernel(const __grid_const
                     }
                     tmem_st_wait();
                 }
-                // (2^7 more than 2^(s - m), at most 2^15: what fp16 cuts off is then 2^-32 of the largest weight, and a million of the smallest count)
-                const float mm = m == -INFINITY ? 0.f : 7.f - m;
+                // (2^4 times 2^(s - m): what fp16 cuts off is then 2^-29 of the largest weight, below what sums of 32 bits lose anyway.  No more than
+                // that: values up to 2^123 stay finite on their way)
+                const float mm = m == -INFINITY ? 0.f : 4.f - m;
                 float2 sum = make_float2(0.f, 0.f);
                 auto weights = [&](auto pair) {
 #pragma unroll
