@@ -437,8 +437,8 @@ int32_t edg_linear_workspace_bytes(const edg_linear_desc* desc, int32_t T, size_
 /* record dev; x dev bf16 [T][ldx], each row 16-byte aligned; A dev bf16 [rank][Kd] and B dev bf16 [N][rank], 16-byte aligned (read only
  * with rank > 0); y dev [T][ldy] of out_dtype, aligned to its type (columns N.. of a row are not touched); workspace 256-byte aligned, needs no
  * initialisation; calls that share one must be ordered on the device.  1 <= T <= 65535; made for batched decode: every 16 tokens, or 8
- * where that is less work, go through the weights once more, so the time of longer calls grows with T.  Codes enter the products exactly, activations as fp16 beside a power of two per token (2^-34 of the
- * largest one is lost), sums are fp32. */
+ * where that is less work, go through the weights once more, so the time of longer calls grows with T.  Codes enter the products exactly,
+ * activations as fp16 beside a power of two per token (2^-34 of the largest one is lost), sums are fp32. */
 int32_t linear_int4_lora(const edg_linear_desc* desc, const void* record, int32_t T, const void* x, const void* A, const void* B,
                          void* y, void* workspace, size_t workspace_bytes, void* stream);
 
@@ -511,9 +511,10 @@ int32_t edg_pages_copy(const edg_page_cache* dst, const edg_page_cache* src, int
  *   absorbed   q_lat = W_uk[h]^T q_nope, o_lat = sum_j p_j c_j, y = W_uv[h] o_lat: reads every cache row once for all heads (decoding)
  *   expanded   keys and values of every head are written out once, then plain attention over them (prompts)
  * Both take bf16 operands with fp32 sums and softmax; q_lat, o_lat (as two bf16 parts) and the weights softmax(s) enter products as bf16 in
- * the absorbed form, the expanded keys in the other: half a bf16 step each, as y itself in bf16 and more than y itself in fp16.  The other's values and weights are fp16 (half a step: 2^-11) in
- * each tile of 128 positions where the magnitudes of its rows and of W_uv show that fp16 holds the values, and bf16 elsewhere.  EDG_LATENT_AUTO takes the
- * form of a sequence by its new rows and by the bounds that a call gives; the results of the two differ by those roundings. */
+ * the absorbed form, the expanded keys in the other: half a bf16 step each, as y itself in bf16 and more than y itself in fp16.  The expanded
+ * values and the weights beside them are fp16 (half a step: 2^-11) in each tile of 128 positions where the magnitudes of its rows and of W_uv
+ * show that fp16 holds the values, and bf16 elsewhere.  EDG_LATENT_AUTO takes the form of a sequence by its new rows and by the bounds that a call
+ * gives; the results of the two differ by those roundings. */
 #define EDG_LATENT_AUTO     0
 #define EDG_LATENT_ABSORBED 1
 #define EDG_LATENT_EXPANDED 2

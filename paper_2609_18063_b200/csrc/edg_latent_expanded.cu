@@ -21,8 +21,8 @@
 //
 // 4,430 new rows of three sequences of 7,103 positions, 32 heads of 128 + 64 / 128, 512 latent columns: 232 to 282 us, by the box; under a
 // profiler the plan and the look through W_uv 5, expand_kernel 64 to 67 (62 GFLOP: 1.0 PFLOP/s; its limits are the weights, which every CTA reads from
-// L2, and its two rounds of CTAs), prompt_kernel 190 (185 GFLOP of rows that see one another: 1.0 PFLOP/s).  A pair of tiles takes 3,900 clocks, with products under way for 3,260 (2,600 by their
-// operations); S of a tile, its softmax (2,050) and P V follow one another, since neither tensor memory has room for a third S nor shared
+// L2, and its two rounds of CTAs), prompt_kernel 190 (185 GFLOP of rows that see one another: 1.0 PFLOP/s).  A pair of tiles takes 3,900
+// clocks, with products under way for 3,260 (2,600 by their operations); S of a tile, its softmax (2,050) and P V follow one another, since neither tensor memory has room for a third S nor shared
 // memory for P.
 #include "edg_latent.cuh"
 #include "edg_umma.cuh"
